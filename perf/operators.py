@@ -103,7 +103,7 @@ def _mx4(w):
     a = v.abs()
     # halfway values go to the even code
     code = ((a > 0.25).to(torch.uint8) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0)
-            + 8 * torch.signbit(v))
+            + 8 * torch.signbit(v).to(torch.uint8))
     return code[:, 0::2] | (code[:, 1::2] << 4), s
 
 
