@@ -260,6 +260,94 @@ int ws_bridge_fusable(int32_t gather_dim, int32_t n_src, const int64_t* src_exte
                       int32_t partition_dim, int32_t n_dst, const int64_t* dst_extents,
                       int32_t* fusable);
 
+/* ---- Around the split layer of a language model: features in, gradients out ----------------------
+ * In a language model the features X of the split layer are token rows that a root-mean-square norm makes of the residual
+ * stream, and dX flows back through it.  Types of the stream: stream_bytes 2 = bf16, 4 = fp32.
+ *
+ * 8 and 4 bits.  "mx" stands for values with one scale for every 32 neighbours along the features: e4m3 (8 bits; largest
+ * value 448) or e2m1 (4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; two to a byte, the first in the low bits) times
+ * 2^(scale byte - 127).  The library picks the smallest power of two that keeps the group's largest magnitude within the
+ * type's range, and rounds to the nearest value, ties to even; a group of zeros has scale byte 0, a group that holds an
+ * infinity or a NaN has scale byte 255, which makes all of it NaN.  Pitches of 8- and 4-bit matrices and of scales are in BYTES;
+ * the matrices 16-byte aligned with pitches that are multiples of 16, scales 2-byte aligned with even pitches >= D / 32.
+ *
+ * Alignment otherwise as above; gamma 16-byte aligned; fp32 matrices may have pitches that are multiples of 4.  D at most
+ * WS_RMS_NORM_MAX_D for the norm, whose kernels hold a row in registers (else WS_ERR_SHAPE). */
+#define WS_RMS_NORM_MAX_D 16384
+
+/* The norm, with the residual's addition in front of it:
+ *   h[i][d] = residual[i][d] + x[i][d], rounded to the stream's type     (residual NULL: h = x)
+ *   rstd[i] = 1 / sqrt(mean_d h[i][d]^2 + eps)                           fp32 sums of the rounded h
+ *   y[i][d] = h[i][d] * rstd[i] * gamma[d]
+ * x bf16 [B][ldx]; residual and h in the stream's type; gamma fp32 [D]; eps > 0 and finite (else WS_ERR_RANGE).
+ * h (the stream behind the addition, which the way back reads) and rstd fp32 [B] are written unless NULL; h may be the
+ * residual's own buffer with the same pitch.  ws_rms_norm_fwd writes y in bf16 [B][ldy], as ws_split_fc_fwd reads it;
+ * ws_rms_norm_fwd_mx8 in 8 bits [B][ldy] with scales [B][lds], rounded once from fp32, as ws_split_fc_w4_* read it. */
+int ws_rms_norm_fwd(const void* x, int64_t ldx, const void* residual, int64_t ldr, int32_t stream_bytes,
+                    const float* gamma, float eps, int32_t B, int32_t D,
+                    void* h, int64_t ldh, void* y, int64_t ldy, float* rstd, void* stream);
+int ws_rms_norm_fwd_mx8(const void* x, int64_t ldx, const void* residual, int64_t ldr, int32_t stream_bytes,
+                        const float* gamma, float eps, int32_t B, int32_t D,
+                        void* h, int64_t ldh, void* y, int64_t ldy, void* y_scales, int64_t lds, float* rstd, void* stream);
+
+/* The way back.  dY fp32 [B][lddy] is the gradient of y as the layer leaves it (dX of ws_split_fc_bwd summed over the shards,
+ * ws_bridge_reduce_partition); h is what the forward call wrote, or x (stream_bytes 2) if there was no residual; rstd its output.
+ *   dh[i][d]  = dres[i][d] + rstd[i] * (g - xhat * mean_d(g * xhat)),  g = gamma[d] * dY[i][d],  xhat = h[i][d] * rstd[i]
+ *   dgamma[d] = sum_i dY[i][d] * xhat[i][d]                                   fp32, in a fixed order of the rows
+ * dh, in the stream's type, is the gradient of x and of the residual alike.  dres, in the same type, is the gradient that
+ * reaches h beside the norm, or NULL; dh may be its buffer with the same pitch.  dgamma NULL: skipped, no workspace needed. */
+size_t ws_rms_norm_bwd_workspace_bytes(int32_t B, int32_t D);
+int ws_rms_norm_bwd(const float* dY, int64_t lddy, const void* h, int64_t ldh, const void* dres, int64_t ldd,
+                    int32_t stream_bytes, const float* gamma, const float* rstd, int32_t B, int32_t D,
+                    void* dh, int64_t lddh, float* dgamma, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The split layer with 4-bit weights, for serving: what a token needs of a shard is bound by reading its weights, and these are
+ * 0.53 bytes each instead of 2.
+ *   ws_quantize_mx4        packs bf16 weights [C][ldw] into codes [C][ldw4] and scales [C][lds]; a shard's rows are its own,
+ *                          so a slice of the packed layer is the packed slice
+ *   ws_split_fc_w4_logits  Z[i][c] = sum_d X[i][d] * W[c][d] + b_shard[c]    fp32 [B][ldz], as ws_sp2_reduce_stats reads it:
+ *                          16-byte aligned, pitch a multiple of 4; columns beyond C_shard are not touched
+ *   ws_split_fc_w4_top1    the arg-max of the same logits, which are not written: outputs, ties and merging over shards as
+ *                          for ws_split_fc_top1 and ws_combine_top1; workspace of ws_w4_top1_workspace_bytes
+ * X_scales NULL: X is bf16 [B][ldx], ldx in elements.  Else X is e4m3 [B][ldx] with scales [B][ldxs].  Weights and features are
+ * multiplied as the values they stand for, with fp32 sums; a product of value and scale beyond bf16's range is not supported.
+ * No matrix is limited to 4 GiB here; at most WS_W4_MAX_ROWS rows to a call (else WS_ERR_SHAPE). */
+#define WS_W4_MAX_ROWS (1 << 20)
+int ws_quantize_mx4(const void* W, int64_t ldw, int32_t C, int32_t D, void* W4, int64_t ldw4,
+                    void* W_scales, int64_t lds, void* stream);
+int ws_split_fc_w4_logits(const void* X, int64_t ldx, const void* X_scales, int64_t ldxs,
+                          const void* W4, int64_t ldw4, const void* W_scales, int64_t lds, const float* b_shard,
+                          int32_t B, int32_t D, int32_t C_shard, float* Z, int64_t ldz, void* stream);
+size_t ws_w4_top1_workspace_bytes(int32_t B, int32_t C_shard);
+int ws_split_fc_w4_top1(const void* X, int64_t ldx, const void* X_scales, int64_t ldxs,
+                        const void* W4, int64_t ldw4, const void* W_scales, int64_t lds, const float* b_shard,
+                        int32_t B, int32_t D, int32_t C_shard, int32_t class_offset, float* top_logit, int32_t* top_class,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* The norm over all gradients of a training step, and clipping by it.  The gradients of a split layer live on different
+ * devices: each device sums the squares of its own, and the norm is taken of the sum of S such parts (S at most
+ * WS_GRAD_MAX_PARTS, else WS_ERR_RANGE), whichever way they were brought together.
+ *   ws_grad_sumsq     sumsq[0] = sum over all tensors of g^2                    fp64, in a fixed order
+ *   ws_grad_clip      norm[0] = sqrt(sum_s sumsq[s]);  g <- k * g,  k = min(1, max_norm / norm)
+ *   ws_grad_clip_sgd  the same k, applied on the way into the weights:  p <- p - lr * (k * g)   in fp32, rounded to p's type; the
+ *                     gradients stay as they are
+ * If the norm is infinite or NaN the step is left out: ws_grad_clip sets every gradient to 0, ws_grad_clip_sgd leaves the weights
+ * unchanged.  norm fp32 [1] or NULL.  max_norm > 0 (infinity never clips); lr finite (else WS_ERR_RANGE).
+ * Tensor i is [rows[i]][cols[i]] with pitch lds[i] (no less than cols[i] if it has more than one row), elem_bytes[i] 2 = bf16 or
+ * 4 = fp32; data pointers need the alignment of their elements only, wider alignment is detected and used.  Parameter i has the
+ * gradient's extents and its own pitch and type.  All tables are HOST arrays of n entries; tensors without elements are
+ * skipped; no two tensors may overlap.  workspace of ws_grad_workspace_bytes(n). */
+#define WS_GRAD_MAX_PARTS 64
+size_t ws_grad_workspace_bytes(int32_t n);
+int ws_grad_sumsq(const void* const* grads, const int64_t* rows, const int64_t* cols, const int64_t* lds,
+                  const int32_t* elem_bytes, int32_t n, double* sumsq, void* workspace, size_t workspace_bytes, void* stream);
+int ws_grad_clip(void* const* grads, const int64_t* rows, const int64_t* cols, const int64_t* lds,
+                 const int32_t* elem_bytes, int32_t n, const double* sumsq, int32_t S, float max_norm, float* norm, void* stream);
+int ws_grad_clip_sgd(void* const* params, const int64_t* ld_params, const int32_t* param_bytes,
+                     const void* const* grads, const int64_t* rows, const int64_t* cols, const int64_t* lds,
+                     const int32_t* elem_bytes, int32_t n, const double* sumsq, int32_t S, float max_norm, float lr,
+                     float* norm, void* stream);
+
 /* ---- The contraction-split sharding pattern, for comparison (Section 3.2.2, Section 5.3.2) --------
  * The paper's MatMul ShardingUnit has two sharding patterns: SP1 cuts the second input along its
  * second dimension (the class split every other entry point of this library implements), SP2 cuts

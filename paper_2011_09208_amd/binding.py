@@ -5,6 +5,7 @@ and takes torch tensors that already live on the GPU; torch is used for device
 memory and the current stream, nothing else.  There is no CPU fallback: if the
 library has not been built, importing this module raises.
 """
+import array
 import ctypes
 import os
 
@@ -88,13 +89,44 @@ lib.ws_sp2_partial_logits.argtypes = [_p, _i64, _p, _i64, _i32, _i32, _i32, _p, 
 lib.ws_sp2_reduce_stats.restype = ctypes.c_int
 lib.ws_sp2_reduce_stats.argtypes = [ctypes.POINTER(_p), ctypes.POINTER(_i64), _i32, _p, _p, _i32, _i32, _p, _p, _p]
 
+lib.ws_rms_norm_fwd.restype = ctypes.c_int
+lib.ws_rms_norm_fwd.argtypes = [_p, _i64, _p, _i64, _i32, _p, _f32, _i32, _i32, _p, _i64, _p, _i64, _p, _p]
+lib.ws_rms_norm_fwd_mx8.restype = ctypes.c_int
+lib.ws_rms_norm_fwd_mx8.argtypes = [_p, _i64, _p, _i64, _i32, _p, _f32, _i32, _i32, _p, _i64, _p, _i64, _p, _i64, _p, _p]
+lib.ws_rms_norm_bwd_workspace_bytes.restype = _sz
+lib.ws_rms_norm_bwd_workspace_bytes.argtypes = [_i32, _i32]
+lib.ws_rms_norm_bwd.restype = ctypes.c_int
+lib.ws_rms_norm_bwd.argtypes = [_p, _i64, _p, _i64, _p, _i64, _i32, _p, _p, _i32, _i32, _p, _i64, _p, _p, _sz, _p]
+
+lib.ws_quantize_mx4.restype = ctypes.c_int
+lib.ws_quantize_mx4.argtypes = [_p, _i64, _i32, _i32, _p, _i64, _p, _i64, _p]
+lib.ws_split_fc_w4_logits.restype = ctypes.c_int
+lib.ws_split_fc_w4_logits.argtypes = [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i32, _i32, _i32, _p, _i64, _p]
+lib.ws_w4_top1_workspace_bytes.restype = _sz
+lib.ws_w4_top1_workspace_bytes.argtypes = [_i32, _i32]
+lib.ws_split_fc_w4_top1.restype = ctypes.c_int
+lib.ws_split_fc_w4_top1.argtypes = [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _p, _i32, _i32, _i32, _i32, _p, _p, _p, _sz, _p]
+
+lib.ws_grad_workspace_bytes.restype = _sz
+lib.ws_grad_workspace_bytes.argtypes = [_i32]
+lib.ws_grad_sumsq.restype = ctypes.c_int
+lib.ws_grad_sumsq.argtypes = [_p, _p, _p, _p, _p, _i32, _p, _p, _sz, _p]
+lib.ws_grad_clip.restype = ctypes.c_int
+lib.ws_grad_clip.argtypes = [_p, _p, _p, _p, _p, _i32, _p, _i32, _f32, _p, _p]
+lib.ws_grad_clip_sgd.restype = ctypes.c_int
+lib.ws_grad_clip_sgd.argtypes = [_p, _p, _p, _p, _p, _p, _p, _p, _i32, _p, _i32, _f32, _f32, _p, _p]
+
 STATIC_SCRATCH_BYTES = 16 << 20
+RMS_NORM_MAX_D = 16384
 
 EXPORTS = ["ws_status_string", "ws_version", "ws_fwd_workspace_bytes", "ws_split_fc_fwd", "ws_split_fc_fwd_static",
            "ws_combine_partials", "ws_bwd_workspace_bytes", "ws_split_fc_bwd", "ws_split_fc_bwd_sgd", "ws_split_fc_predict", "ws_split_fc_top1", "ws_combine_top1",
            "ws_profile_enable", "ws_profile_reset", "ws_profile_pause", "ws_profile_trace_dw", "ws_profile_kernel_count", "ws_profile_kernel_name",
            "ws_profile_read", "ws_balance_widths",
            "ws_bridge_gather", "ws_bridge_reduce_partition", "ws_bridge_fusable",
+           "ws_rms_norm_fwd", "ws_rms_norm_fwd_mx8", "ws_rms_norm_bwd_workspace_bytes", "ws_rms_norm_bwd",
+           "ws_quantize_mx4", "ws_split_fc_w4_logits", "ws_w4_top1_workspace_bytes", "ws_split_fc_w4_top1",
+           "ws_grad_workspace_bytes", "ws_grad_sumsq", "ws_grad_clip", "ws_grad_clip_sgd",
            "ws_sp2_partial_logits", "ws_sp2_reduce_stats", "ws_probe_mfma_loop", "ws_probe_gemm"]
 
 
@@ -316,6 +348,171 @@ def bridge_fusable(gather_dim, src_extents, partition_dim, dst_extents):
     _check(lib.ws_bridge_fusable(int(gather_dim), len(src_extents), a, int(partition_dim), len(dst_extents), b,
                                  ctypes.byref(ok)))
     return bool(ok.value)
+
+
+def _pitch(t, rows, cols, elem_bytes):
+    """Row pitch of a [rows, cols] device tensor whose rows are contiguous; None for no tensor."""
+    if t is None:
+        return 0
+    shape = t.shape
+    assert len(shape) == 2 and shape[0] == rows and shape[1] == cols and t.element_size() == elem_bytes and t.is_cuda
+    ld, unit = t.stride()
+    assert unit == 1 or cols == 1
+    return ld if rows > 1 else max(ld, cols)
+
+
+def _vector(t, n, dtype):
+    assert t is None or (t.shape == (n,) and t.dtype == dtype and t.is_contiguous() and t.is_cuda)
+    return None if t is None else t.data_ptr()
+
+
+_STREAM_TYPES = {torch.bfloat16: 2, torch.float32: 4}
+
+
+def _stream_bytes(*tensors):
+    """Bytes of the residual stream's type: the one that the given tensors (or None) share, bf16 if there is none."""
+    types = {t.dtype for t in tensors if t is not None}
+    assert len(types) <= 1
+    return _STREAM_TYPES[types.pop()] if types else 2
+
+
+def rms_norm_fwd(x, residual, gamma, eps, h, y, rstd):
+    """h = residual + x, y = h * rstd * gamma.  x, y bf16 [B, D]; residual, h bf16 or fp32 [B, D] or None; gamma fp32 [D];
+    rstd fp32 [B] or None.  h may be residual itself."""
+    B, D = x.shape
+    es = _stream_bytes(residual, h)
+    assert x.dtype == torch.bfloat16 and y.dtype == torch.bfloat16
+    _check(lib.ws_rms_norm_fwd(x.data_ptr(), _pitch(x, B, D, 2), _ptr(residual), _pitch(residual, B, D, es), es, _vector(gamma, D, torch.float32),
+                               eps, B, D, _ptr(h), _pitch(h, B, D, es), y.data_ptr(), _pitch(y, B, D, 2), _vector(rstd, B, torch.float32),
+                               _stream()))
+
+
+def rms_norm_fwd_mx8(x, residual, gamma, eps, h, y, y_scales, rstd):
+    """rms_norm_fwd with y in 8 bits: y uint8 or float8_e4m3fn [B, D], y_scales uint8 [B, D / 32]."""
+    B, D = x.shape
+    es = _stream_bytes(residual, h)
+    assert x.dtype == torch.bfloat16
+    _check(lib.ws_rms_norm_fwd_mx8(x.data_ptr(), _pitch(x, B, D, 2), _ptr(residual), _pitch(residual, B, D, es), es,
+                                   _vector(gamma, D, torch.float32), eps, B, D, _ptr(h), _pitch(h, B, D, es), y.data_ptr(), _pitch(y, B, D, 1),
+                                   y_scales.data_ptr(), _pitch(y_scales, B, D // 32, 1), _vector(rstd, B, torch.float32), _stream()))
+
+
+def rms_norm_bwd_workspace_bytes(B, D):
+    return lib.ws_rms_norm_bwd_workspace_bytes(B, D)
+
+
+def rms_norm_bwd(dY, h, dres, gamma, rstd, dh, dgamma, workspace):
+    """dY fp32 [B, D]; h, dh and dres (or None) bf16 or fp32 [B, D]; gamma fp32 [D]; rstd fp32 [B]; dgamma fp32 [D], or None: then
+    workspace may be None, else it has rms_norm_bwd_workspace_bytes.  dh may be dres itself."""
+    B, D = dY.shape
+    es = _stream_bytes(h, dres, dh)
+    _check(lib.ws_rms_norm_bwd(dY.data_ptr(), _pitch(dY, B, D, 4), h.data_ptr(), _pitch(h, B, D, es), _ptr(dres), _pitch(dres, B, D, es), es,
+                               _vector(gamma, D, torch.float32), _vector(rstd, B, torch.float32), B, D, dh.data_ptr(), _pitch(dh, B, D, es),
+                               _vector(dgamma, D, torch.float32), _ptr(workspace),
+                               0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+
+
+def quantize_mx4(W, W4, W_scales):
+    """W bf16 [C, D] -> W4 uint8 [C, D / 2] (two codes to a byte, the first in the low bits), W_scales uint8 [C, D / 32]."""
+    C, D = W.shape
+    assert W.dtype == torch.bfloat16
+    _check(lib.ws_quantize_mx4(W.data_ptr(), _pitch(W, C, D, 2), C, D, W4.data_ptr(), _pitch(W4, C, D // 2, 1), W_scales.data_ptr(),
+                               _pitch(W_scales, C, D // 32, 1), _stream()))
+
+
+def _w4_args(X, X_scales, W4, W_scales, b_shard):
+    B, D = X.shape
+    C = W4.shape[0]
+    assert X.dtype == torch.bfloat16 or X_scales is not None
+    return (X.data_ptr(), _pitch(X, B, D, 2 if X_scales is None else 1), _ptr(X_scales), _pitch(X_scales, B, D // 32, 1), W4.data_ptr(),
+            _pitch(W4, C, D // 2, 1), W_scales.data_ptr(), _pitch(W_scales, C, D // 32, 1), _vector(b_shard, C, torch.float32), B, D, C)
+
+
+def split_fc_w4_logits(X, X_scales, W4, W_scales, b_shard, Z):
+    """Z fp32 [B, C_shard] (row pitch a multiple of 4) <- X . W^T + b.  X bf16 [B, D] with X_scales None, or uint8 / float8_e4m3fn with
+    X_scales uint8 [B, D / 32]; W4, W_scales as quantize_mx4 leaves them; b_shard fp32 [C_shard] or None."""
+    assert Z.dtype == torch.float32
+    a = _w4_args(X, X_scales, W4, W_scales, b_shard)
+    _check(lib.ws_split_fc_w4_logits(*a, Z.data_ptr(), _pitch(Z, a[9], a[11], 4), _stream()))
+
+
+def w4_top1_workspace_bytes(B, C_shard):
+    return lib.ws_w4_top1_workspace_bytes(B, C_shard)
+
+
+def split_fc_w4_top1(X, X_scales, W4, W_scales, b_shard, class_offset, top_logit, top_class, workspace):
+    """top_logit fp32 [B], top_class int32 [B] <- the shard's best class per row; inputs as split_fc_w4_logits."""
+    a = _w4_args(X, X_scales, W4, W_scales, b_shard)
+    _check(lib.ws_split_fc_w4_top1(*a, int(class_offset), _vector(top_logit, a[9], torch.float32), _vector(top_class, a[9], torch.int32),
+                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
+
+
+def _address(values, code="q"):
+    """(address, owner) of the values as a C array; the owner has to outlive the call."""
+    a = array.array(code, values)
+    return a.buffer_info()[0], a
+
+
+class grad_table:
+    """The tables that grad_sumsq, grad_clip and grad_clip_sgd take, of bf16 or fp32 device tensors that are contiguous, or
+    matrices with contiguous rows.  It holds addresses: build it again when tensors move."""
+
+    def __init__(self, tensors):
+        tensors = list(tensors)
+        self.n = len(tensors)
+        elem_bytes = [_STREAM_TYPES[t.dtype] for t in tensors]
+        rows, cols, lds = [], [], []
+        for t in tensors:
+            if t.dim() == 2:
+                (r, c), (ld, unit) = t.shape, t.stride()
+                assert unit == 1 or c <= 1
+                rows.append(r)
+                cols.append(c)
+                lds.append(ld if r > 1 else c)
+            else:
+                assert t.is_contiguous()
+                n = t.numel()
+                rows.append(1)
+                cols.append(n)
+                lds.append(n)
+        assert all(t.is_cuda for t in tensors)
+        self.extents = (rows, cols)
+        (self.data, a), (self.rows, b), (self.cols, c), (self.lds, d), (self.bytes, e) = (
+            _address([t.data_ptr() for t in tensors]), _address(rows), _address(cols), _address(lds),
+            _address(elem_bytes, "i"))
+        self._owners = (a, b, c, d, e)
+
+
+def _table(tensors):
+    return tensors if isinstance(tensors, grad_table) else grad_table(tensors)
+
+
+def grad_workspace_bytes(n):
+    return lib.ws_grad_workspace_bytes(n)
+
+
+def grad_sumsq(grads, sumsq, workspace):
+    """sumsq fp64 [1] <- the sum of the squares of all gradients (tensors, or their grad_table)."""
+    g = _table(grads)
+    _check(lib.ws_grad_sumsq(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, 1, torch.float64), _ptr(workspace),
+                             workspace.numel() * workspace.element_size(), _stream()))
+
+
+def grad_clip(grads, sumsq, max_norm, norm=None):
+    """Scales the gradients in place by min(1, max_norm / norm), norm = sqrt(sum of sumsq fp64 [S]); norm fp32 [1] or None."""
+    g = _table(grads)
+    S = sumsq.numel()
+    _check(lib.ws_grad_clip(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, torch.float64), S, float(max_norm),
+                            _vector(norm, 1, torch.float32), _stream()))
+
+
+def grad_clip_sgd(params, grads, sumsq, max_norm, lr, norm=None):
+    """params[i] <- params[i] - lr * k * grads[i] with grad_clip's factor k; the gradients are left as they are."""
+    p, g = _table(params), _table(grads)
+    S = sumsq.numel()
+    assert p.extents == g.extents
+    _check(lib.ws_grad_clip_sgd(p.data, p.lds, p.bytes, g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, torch.float64), S,
+                                float(max_norm), float(lr), _vector(norm, 1, torch.float32), _stream()))
 
 
 def sp2_partial_logits(X_slice, W_slice, Z_partial):

@@ -8,8 +8,12 @@ SRC = os.path.join(PKG, "csrc", "whalesplit.hip")
 BRIDGE_SRC = os.path.join(PKG, "csrc", "bridge.hip")
 SP2_SRC = os.path.join(PKG, "csrc", "sp2.hip")
 PROBE_SRC = os.path.join(PKG, "csrc", "probe.hip")
+NORM_SRC = os.path.join(PKG, "csrc", "norm.hip")
+W4_SRC = os.path.join(PKG, "csrc", "w4.hip")
+GRADS_SRC = os.path.join(PKG, "csrc", "grads.hip")
 HOST_SRC = os.path.join(PKG, "csrc", "balance.cpp")
-DEPS = [SRC, BRIDGE_SRC, SP2_SRC, PROBE_SRC, HOST_SRC, os.path.join(PKG, "csrc", "gemm_core.h"), os.path.join(PKG, "csrc", "gemm_stream.h"),
+SRCS = [SRC, BRIDGE_SRC, SP2_SRC, PROBE_SRC, NORM_SRC, W4_SRC, GRADS_SRC, HOST_SRC]
+DEPS = SRCS + [os.path.join(PKG, "csrc", "mx.h"), os.path.join(PKG, "csrc", "gemm_core.h"), os.path.join(PKG, "csrc", "gemm_stream.h"),
         os.path.join(PKG, "csrc", "gemm_small.h"), os.path.join(PKG, "csrc", "gemm_block.h"),
         os.path.join(PKG, "csrc", "gemm_tiles.h"), os.path.join(PKG, "csrc", "plan.h"),
         os.path.join(os.path.dirname(PKG), "include", "whalesplit.h")]
@@ -30,7 +34,7 @@ HOST_PASS_NOTE = "'-packed-fp32-ops' is not a recognized feature for this target
 
 
 def build(verbose=False, extra=()):
-    cmd = [HIPCC, *FLAGS, *extra, SRC, BRIDGE_SRC, SP2_SRC, PROBE_SRC, HOST_SRC, "-o", LIB]
+    cmd = [HIPCC, *FLAGS, *extra, *SRCS, "-o", LIB]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

@@ -476,6 +476,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, r);
 }
 
+// The better of two (logit, class) candidates: the larger logit, the lower class id among equals.
+__device__ __forceinline__ void better_of(float& v, int& c, float v2, int c2) {
+    if (v2 > v || (v2 == v && c2 < c)) {
+        v = v2;
+        c = c2;
+    }
+}
+
 // ---- output tiles through LDS ------------------------------------------------------------------------
 // The MFMA accumulator layout gives a lane one N index and groups of four consecutive M indices, which
 // makes direct global stores 8 or 16 bytes wide and scattered over 16 rows.  Instead the 256 x 256 tile

@@ -1101,14 +1101,6 @@ __global__ __launch_bounds__(NTHREADS) void predict_probs(FcArgs a, const float*
 }
 
 // ---- arg-max predictions --------------------------------------------------------------------------
-// The better of two (logit, class) candidates: the larger logit, the lower class id among equals.
-__device__ __forceinline__ void better_of(float& v, int& c, float v2, int c2) {
-    if (v2 > v || (v2 == v && c2 < c)) {
-        v = v2;
-        c = c2;
-    }
-}
-
 // Top-1 of every row over one 256-class tile: the logits GEMM of fwd_logits_stats with an arg-max
 // epilogue.  Partial (logit, shard-local class) pairs go to part_val / part_cls [class tile][row].
 __global__ __launch_bounds__(NTHREADS) void top1_logits(FcArgs a, float* __restrict__ part_val,

@@ -1,0 +1,211 @@
+"""GPU: the operators around the split layer used together with it, as a language model's last block does: a training step from the
+residual stream to updated weights, and the answer to a batch of tokens with 4-bit weights; eager, on another stream and captured."""
+import numpy as np
+import pytest
+
+from tests import mx_formats as mx
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU; there is no CPU fallback")
+    return torch
+
+
+EPS, LR = 1e-5, 0.5
+
+
+class Training:
+    """One step of norm, split layer (two shards), way back, norm of the gradients and clipped update."""
+
+    def __init__(self, torch, B, D, widths, limit, seed):
+        from paper_2011_09208_amd import binding as ws
+        dev, C = "cuda", sum(widths)
+        g = torch.Generator(device=dev).manual_seed(seed)
+        self.B, self.D, self.widths, self.limit = B, D, widths, limit
+        self.x = torch.randn((B, D), device=dev, generator=g).to(torch.bfloat16)
+        self.res = 2 * torch.randn((B, D), device=dev, generator=g)
+        self.gamma = 1 + 0.2 * torch.randn(D, device=dev, generator=g)
+        self.W = (0.05 * torch.randn((C, D), device=dev, generator=g)).to(torch.bfloat16)
+        self.b = 0.1 * torch.randn(C, device=dev, generator=g)
+        self.y = torch.randint(0, C, (B,), device=dev, generator=g, dtype=torch.int32)
+        f = lambda *s, dtype=torch.float32: torch.empty(s, device=dev, dtype=dtype)                 # noqa: E731
+        self.h, self.X, self.rstd = f(B, D), f(B, D, dtype=torch.bfloat16), f(B)
+        self.m, self.s, self.t, self.lse, self.loss, self.mean = f(2, B), f(2, B), f(2, B), f(B), f(B), f(1)
+        self.dX, self.dW, self.db, self.dh, self.dgamma = f(B, D), f(C, D, dtype=torch.bfloat16), f(C), f(B, D), f(D)
+        self.sumsq, self.norm = f(1, dtype=torch.float64), f(1)
+        n = max(max(ws.fwd_workspace_bytes(B, D, w), ws.bwd_workspace_bytes(B, D, w)) for w in widths)
+        n = max(n, ws.rms_norm_bwd_workspace_bytes(B, D), ws.grad_workspace_bytes(6))
+        self.work = f(n, dtype=torch.uint8)
+
+    def step(self):
+        from paper_2011_09208_amd import binding as ws
+        a, cut = self, self.widths[0]
+        parts = ((0, a.W[:cut], a.b[:cut], a.dW[:cut], a.db[:cut]), (cut, a.W[cut:], a.b[cut:], a.dW[cut:], a.db[cut:]))
+        ws.rms_norm_fwd(a.x, a.res, a.gamma, EPS, a.h, a.X, a.rstd)
+        for i, (off, W, b, _, _) in enumerate(parts):
+            ws.split_fc_fwd(a.X, W, b, a.y, off, a.m[i], a.s[i], a.t[i], a.work)
+        ws.combine_partials(a.m, a.s, a.t, a.lse, a.loss, a.mean)
+        for i, (off, W, b, dW, db) in enumerate(parts):
+            ws.split_fc_bwd(a.X, W, b, a.lse, a.y, off, 1.0 / a.B, a.dX, i > 0, dW, db, a.work)
+        ws.rms_norm_bwd(a.dX, a.h, None, a.gamma, a.rstd, a.dh, a.dgamma, a.work)
+        grads = [dW for _, _, _, dW, _ in parts] + [db for _, _, _, _, db in parts] + [a.dgamma]
+        ws.grad_sumsq(grads, a.sumsq, a.work)
+        params = [W for _, W, _, _, _ in parts] + [b for _, _, b, _, _ in parts] + [a.gamma]
+        ws.grad_clip_sgd(params, grads, a.sumsq, a.limit, LR, a.norm)
+
+    def outputs(self):
+        return [t.clone() for t in (self.mean, self.dh, self.dgamma, self.norm, self.W, self.b, self.gamma)]
+
+
+def _near(got, want, what):
+    """Within 2e-2 of the largest magnitude: X, dz and dW are rounded to bf16 on the way, half a step of 2^-8 each."""
+    err = float((got.double() - want).abs().max() / want.abs().max())
+    assert err <= 2e-2, (what, err)
+
+
+@pytest.mark.parametrize("B,D,widths", [(37, 192, (300, 201)), (300, 1024, (1500, 523))])
+@pytest.mark.parametrize("limit", [0.05, 100.0])
+def test_training_step(torch, B, D, widths, limit):
+    a = Training(torch, B, D, widths, limit, B)
+    h, gamma, W, b = (v.double() for v in (a.x.float() + a.res, a.gamma, a.W, a.b))
+    leaves = [v.requires_grad_() for v in (h, gamma, W, b)]
+    X = h / torch.sqrt((h * h).mean(1, keepdim=True) + EPS) * gamma
+    z = X @ W.t() + b
+    loss = (torch.logsumexp(z, 1) - z[torch.arange(B, device="cuda"), a.y.long()]).mean()
+    dh, dgamma, dW, db = torch.autograd.grad(loss, leaves)
+    norm = torch.sqrt((dgamma ** 2).sum() + (dW ** 2).sum() + (db ** 2).sum())
+    k = min(1.0, limit / float(norm))
+    gamma0, W0, b0 = a.gamma.double(), a.W.double(), a.b.double()
+    a.step()
+    assert abs(float(a.mean) - float(loss)) <= 1e-3 * float(loss)
+    _near(a.dh, dh, "dh"), _near(a.dgamma, dgamma, "dgamma"), _near(a.dW, dW, "dW"), _near(a.db, db, "db")
+    assert abs(float(a.norm) - float(norm)) <= 2e-2 * float(norm)
+    # the update that was made, but for the rounding of the new weights
+    assert ((a.gamma.double() - gamma0) + LR * k * dgamma).abs().max() <= 4e-2 * LR * k * dgamma.abs().max() + 2.0 ** -24 * 2
+    assert ((a.b.double() - b0) + LR * k * db).abs().max() <= 4e-2 * LR * k * db.abs().max() + 2.0 ** -24
+    assert (((a.W.double() - W0) + LR * k * dW).abs() <= 4e-2 * LR * k * dW.abs().max() + 2.0 ** -8 * (W0.abs() + LR * k * dW.abs())).all()
+
+
+class Serving:
+    def __init__(self, torch, B, D, widths, seed):
+        from paper_2011_09208_amd import binding as ws
+        dev, C = "cuda", sum(widths)
+        g = torch.Generator(device=dev).manual_seed(seed)
+        self.widths = widths
+        self.x = torch.randn((B, D), device=dev, generator=g).to(torch.bfloat16)
+        self.res = (2 * torch.randn((B, D), device=dev, generator=g)).to(torch.bfloat16)
+        self.gamma = 1 + 0.2 * torch.randn(D, device=dev, generator=g)
+        W = (0.05 * torch.randn((C, D), device=dev, generator=g)).to(torch.bfloat16)
+        self.b = 0.1 * torch.randn(C, device=dev, generator=g)
+        u8 = lambda *s: torch.empty(s, device=dev, dtype=torch.uint8)                               # noqa: E731
+        self.W4, self.Ws, self.q, self.qs = u8(C, D // 2), u8(C, D // 32), u8(B, D), u8(B, D // 32)
+        ws.quantize_mx4(W, self.W4, self.Ws)
+        self.top, self.cls = torch.empty((2, B), device=dev), torch.empty((2, B), device=dev, dtype=torch.int32)
+        self.best, self.best_cls = torch.empty(B, device=dev), torch.empty(B, device=dev, dtype=torch.int32)
+        self.Z = torch.empty((B, (C + 3) // 4 * 4), device=dev)[:, :C]
+        self.y = torch.randint(0, C, (B,), device=dev, generator=g, dtype=torch.int32)
+        self.lse, self.loss = torch.empty(B, device=dev), torch.empty(B, device=dev)
+        self.work = [u8(ws.w4_top1_workspace_bytes(B, w)) for w in widths]
+
+    def step(self):
+        from paper_2011_09208_amd import binding as ws
+        a, cut = self, self.widths[0]
+        ws.rms_norm_fwd_mx8(a.x, a.res, a.gamma, EPS, a.res, a.q, a.qs, None)                       # the stream in place
+        for i, sl in enumerate((slice(0, cut), slice(cut, None))):
+            ws.split_fc_w4_top1(a.q, a.qs, a.W4[sl], a.Ws[sl], a.b[sl], i * cut, a.top[i], a.cls[i], a.work[i])
+        ws.combine_top1(a.top, a.cls, a.best, a.best_cls)
+        ws.split_fc_w4_logits(a.q, a.qs, a.W4, a.Ws, a.b, a.Z)
+        ws.sp2_reduce_stats([a.Z], None, a.y, a.lse, a.loss)                                        # probabilities: exp(Z - lse)
+
+    def outputs(self):
+        return [t.clone() for t in (self.res, self.q, self.qs, self.best, self.best_cls, self.Z, self.lse, self.loss)]
+
+
+@pytest.mark.parametrize("B,D,widths", [(1, 256, (130, 71)), (33, 1088, (900, 1333))])
+def test_answering_tokens(torch, B, D, widths):
+    a = Serving(torch, B, D, widths, B)
+    a.step()
+    W = mx.values4(a.W4.cpu().numpy(), a.Ws.cpu().numpy())
+    X = mx.values8(a.q.cpu().numpy(), a.qs.cpu().numpy())
+    z = X @ W.T + a.b.double().cpu().numpy()
+    slack = (D / 32 + 48) * 2.0 ** -23 * (np.abs(X) @ np.abs(W).T + 1.0).max()                      # fp32 sums of exact products
+    Z = a.Z.double().cpu().numpy()
+    assert np.abs(Z - z).max() <= slack
+    at, r = a.best_cls.cpu().numpy(), np.arange(B)
+    assert np.all(z[r, at] >= z.max(1) - 2 * slack) and np.abs(a.best.double().cpu().numpy() - z[r, at]).max() <= slack
+    lse = np.log(np.exp(z - z.max(1, keepdims=True)).sum(1)) + z.max(1)
+    assert np.abs(a.lse.double().cpu().numpy() - lse).max() <= slack + 2e-5
+    assert np.abs(a.loss.double().cpu().numpy() - (lse - z[r, a.y.cpu().numpy()])).max() <= 2 * slack + 2e-5
+
+
+def _state(a, torch):
+    return {k: v.clone() for k, v in vars(a).items() if isinstance(v, torch.Tensor)}
+
+
+def _restore(a, state):
+    for k, v in state.items():
+        getattr(a, k).copy_(v)
+
+
+@pytest.mark.parametrize("make", [lambda t: Training(t, 70, 320, (500, 77), 0.05, 3), lambda t: Serving(t, 5, 576, (400, 233), 4),
+                                  lambda t: Serving(t, 1, 4160, (4000, 65), 5)], ids=["training", "serving", "one token"])
+def test_captured_and_on_another_stream(torch, make):
+    """Replays of a captured step, with eager work and new inputs between them, give what eager steps give, bit for bit."""
+    a = make(torch)
+    start = _state(a, torch)
+    a.step()
+    torch.cuda.synchronize()
+    want = a.outputs()
+    side = torch.cuda.Stream()
+    _restore(a, start)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        a.step()
+        got = a.outputs()
+    side.synchronize()
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
+    _restore(a, start)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step()
+    for turn in range(4):
+        _restore(a, start)
+        a.x.mul_(1.0 + 0.5 * turn)                        # other inputs each time
+        graph.replay()
+        torch.cuda.synchronize()
+        got = a.outputs()
+        _restore(a, start)
+        a.x.mul_(1.0 + 0.5 * turn)
+        a.step()
+        torch.cuda.synchronize()
+        want = a.outputs()
+        assert all(torch.equal(g, w) for g, w in zip(got, want)), turn
+
+
+def test_two_streams_at_once(torch):
+    """Two callers with their own buffers on their own streams do not disturb each other."""
+    a, b = (Serving(torch, 3, 1024, (3000, 700), s) for s in (6, 7))
+    start = [_state(a, torch), _state(b, torch)]
+    want = []
+    for o in (a, b):
+        o.step()
+        torch.cuda.synchronize()
+        want.append(o.outputs())
+    for o, s in zip((a, b), start):
+        _restore(o, s)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for turn in range(3):
+        for o, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                _restore(o, start[0 if o is a else 1])
+                o.step()
+    torch.cuda.synchronize()
+    for o, w in zip((a, b), want):
+        assert all(torch.equal(g, v) for g, v in zip(o.outputs(), w))
