@@ -53,27 +53,260 @@ struct W4Args {
     const float* bias;
     int B, D, C;
     float* Z; int64_t ldz;
-    float* part_val; int* part_cls; int class_offset;
+    float* part_val; int* part_cls;          // [B][workgroups along the classes]
 };
 
-constexpr int W4_SPAN = 512;                 // features that the lanes of a wave cover with four pieces of 32 each
-constexpr int W4_WAVES = 4;
 constexpr int W4_MAX_ROWS = WS_W4_MAX_ROWS;  // row tiles are counted in the grid's second extent
+constexpr int64_t W4_MAX_PITCH = 1 << 26;      // 16 rows are addressed with 31 bits
+constexpr int W4_STEP = 128;                 // features that the lanes of a wave cover with 16 bytes of codes each
 
-// A wave takes CT x 16 classes and NT x 16 rows.  Lane l holds class l % 16 (and row l % 16); of every span of 512 features it
-// takes the 128 from 128 (l / 16) on, 32 at a time: 16 bytes of weights, whose four scales are neighbours.  Which features a matrix
-// instruction sums over is free as long as both operands agree.
-template <int NT, int CT, bool MX, bool TOP1>
-__global__ __launch_bounds__(64 * W4_WAVES) void w4_product(W4Args a, int chunk, int groups) {
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+// How a call is cut: a wave takes CT x 16 classes and NT x 16 rows, a workgroup WAVES waves along the classes; the codes of PIECE steps
+// are loaded while those of the PIECE before are multiplied.
+template <int NT_> struct W4Shape {
+    static constexpr int NT = NT_;
+    static constexpr int CT = NT <= 2 ? 1 : 2;
+    static constexpr int WAVES = NT <= 2 ? 4 : 8;
+    static constexpr int PIECE = NT <= 2 ? 4 : NT <= 4 ? 2 : 1;
+    static constexpr int ROWS = 16 * NT, THREADS = 64 * WAVES, CLASSES = 16 * CT * WAVES;
+};
+
+// Steps of `rows` rows of features that 80 KiB hold, so that two workgroups share a compute unit.
+constexpr int W4_LDS = 81920;
+constexpr int w4_chunk(int rows) { return ((W4_LDS / 4 - 256) / rows - 16) / 64; }
+
+// Where a lane loads and where its data goes.  A load takes 16 bytes of codes a lane, four neighbouring lanes 64 bytes of a class row: 16 rows x 64
+// bytes, one step of 16 classes.  With a lane for each row, as the matrix instruction has them, every lane is in a cache line of its own and
+// the addresses of a load take four times as long.  For the product lane l holds class l % 16 and the 32 features from 32 (l / 16) on, which
+// the lanes fetch from each other; which features an instruction sums over is free as long as both operands agree.
+struct W4Lane {
+    int i16, g;                              // of the product: class (and row) and group of 32 features
+    int seg;                                 // of a load: 16-byte piece of class row lane / 4
+    int codes, scale;                        // byte offsets of the lanes to fetch from: codes, and the scales of step 0
+    int turn;                                // brings scale byte g of a step's four to a float's exponent
+    int code_offset, scale_offset;           // of a load, from the tile's first byte
+    __device__ __forceinline__ W4Lane(int lane, const W4Args& a)
+        : i16(lane & 15), g(lane >> 4), seg(lane & 3), codes(4 * (4 * (lane & 15) + (lane >> 4))), scale(16 * (lane & 15)),
+          turn((8 * (lane >> 4) + 9) & 31), code_offset((lane >> 2) * (int)a.ldw + 16 * (lane & 3)), scale_offset((lane >> 2) * (int)a.lds) {}
+};
+
+// Sixteen class rows of codes and of scales as buffers: what lies beyond the last class reads as zeros, without a branch.  A branch around
+// loads, even one that is never taken, makes the compiler wait for them as if nothing had been loaded since.
+struct W4Tile {
+    __amdgpu_buffer_rsrc_t codes, scales;
+    // classes [cls, cls + 16) of the shard; none of them if cls >= C
+    __device__ __forceinline__ W4Tile(const W4Args& a, int cls) {
+        const int64_t n = a.C - cls < 16 ? a.C - cls : 16;
+        const int64_t at = n > 0 ? cls : 0;
+        const int code_bytes = n > 0 ? (int)((n - 1) * a.ldw + (a.D >> 1)) : 0, scale_bytes = n > 0 ? (int)((n - 1) * a.lds + (a.D >> 5)) : 0;
+        codes = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.W + at * a.ldw), 0, code_bytes, 0x00020000);
+        scales = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.ws + at * a.lds), 0, scale_bytes, 0x00020000);
+    }
+};
+
+// Codes and scales of N steps of a tile; of the scales, lane l holds steps l % 4, l % 4 + 4, ..
+template <int N> struct W4Piece {
+    static constexpr int HELD = (N + 3) / 4;
+    u32x4 v[N];
+    uint32_t s[HELD], t[HELD];               // two scales each
+};
+
+// From feature k on (a step's first).  Beyond the row's end it may read the next row's bytes: codes stand for numbers whatever they are, and the
+// features there are zeros; scales are masked when they are used.
+template <int N>
+__device__ __forceinline__ void w4_load(W4Piece<N>& p, const W4Tile& tile, const W4Lane& l, int k) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p.v[i] = __builtin_amdgcn_raw_buffer_load_b128(tile.codes, l.code_offset + 64 * i, k >> 1, 0);
+#pragma unroll
+    for (int j = 0; j < W4Piece<N>::HELD; ++j) {
+        const int off = l.scale_offset + 4 * (N >= 4 ? 4 * j + l.seg : l.seg & (N - 1));
+        p.s[j] = __builtin_amdgcn_raw_buffer_load_b16(tile.scales, off, k >> 5, 0);
+        p.t[j] = __builtin_amdgcn_raw_buffer_load_b16(tile.scales, off + 2, k >> 5, 0);
+    }
+}
+
+// The two halves of four scales.  In assembly: an ordinary expression is moved up to right behind the loads, and waits for them there.
+template <int N>
+__device__ __forceinline__ void w4_join(uint32_t (&joined)[W4Piece<N>::HELD], const W4Piece<N>& p) {
+#pragma unroll
+    for (int j = 0; j < W4Piece<N>::HELD; ++j) asm volatile("v_lshl_or_b32 %0, %1, 16, %2" : "=v"(joined[j]) : "v"(p.t[j]), "v"(p.s[j]));
+}
+
+// The lane's codes and scale of step i for the product, of which `left` features from step 0 on are there (a multiple of 64).
+template <int N>
+__device__ __forceinline__ u32x4 w4_codes(const W4Piece<N>& p, int i, const W4Lane& l) {
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (uint32_t)__builtin_amdgcn_ds_bpermute(l.codes, (int)p.v[i][e]);
+    return v;
+}
+template <bool WHOLE, int HELD>
+__device__ __forceinline__ float w4_scale(const uint32_t (&joined)[HELD], int i, int left, const W4Lane& l) {
+    const uint32_t four = (uint32_t)__builtin_amdgcn_ds_bpermute(l.scale + 4 * (i & 3), (int)joined[i >> 2]);
+    const uint32_t f = __builtin_amdgcn_alignbit(four, four, l.turn);
+    return __uint_as_float(WHOLE || W4_STEP * i + 32 * l.g < left ? f : 0u);
+}
+
+// Eight e4m3 values as bf16, times the scale.
+__device__ __forceinline__ u32x4 w4_features(uint32_t a, uint32_t b, float scale) {
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true))};
+}
+
+// Features of rows [row0, row0 + rows), [k0, k0 + 128 steps), as bf16 into LDS: plane g of four holds the 32 features that lane group g
+// reads of every step, [row][step] with a pitch of an odd number of 16-byte chunks, so that the 16 rows of a read differ in their banks (the
+// planes are whole 256 bytes apart).  Zeros stand for features beyond D.
+template <int THREADS, bool MX>
+__device__ __forceinline__ void w4_stage(const W4Args& a, int row0, int rows, int k0, int steps, char* lds, int pitch, int plane) {
+    const int units = steps * (W4_STEP / 16), left = a.D - k0;
+    for (int u = threadIdx.x; u < rows * units; u += THREADS) {
+        const int r = u / units, c = u - r * units;                            // 16 features from 16 c on
+        u32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+        if (16 * c < left) {
+            const int64_t row = row0 + r;
+            if constexpr (MX) {
+                const u32x4 v = *reinterpret_cast<const u32x4*>(a.X + row * a.ldx + k0 + 16 * c);
+                const float s = scale_of(a.xs[row * a.ldxs + (k0 >> 5) + (c >> 1)], 0);
+                lo = w4_features(v[0], v[1], s);
+                hi = w4_features(v[2], v[3], s);
+            } else {
+                const u32x4* p = reinterpret_cast<const u32x4*>(a.X + row * a.ldx + 2 * k0 + 32 * c);
+                lo = p[0];
+                hi = p[1];
+            }
+        }
+        u32x4* q = reinterpret_cast<u32x4*>(lds + ((c >> 1) & 3) * plane + r * pitch + (c >> 3) * 64 + (c & 1) * 32);
+        q[0] = lo;
+        q[1] = hi;
+    }
+}
+
+// Eight codes as bf16, times the scale.
+__device__ __forceinline__ bf16x8 w4_values(uint32_t codes, float scale) {
+    return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
+                                            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
+                                            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
+                                            __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))});
+}
+
+// acc += codes x features of `left` (at most PIECE steps) features; x[n] points at the lane's row of its plane, at the piece's first step.
+template <bool WHOLE, int CT, int PIECE, int NT>
+__device__ __forceinline__ void w4_multiply_steps(f32x4 (&acc)[CT][NT], const W4Piece<PIECE> (&p)[CT], const char* const (&x)[NT], int at, int left,
+                                                  const W4Lane& l) {
+    uint32_t joined[CT][W4Piece<PIECE>::HELD];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) w4_join(joined[c], p[c]);
+#pragma unroll
+    for (int i = 0; i < PIECE; ++i) {
+        if (!WHOLE && W4_STEP * i >= left) break;
+        float f[CT];
+        u32x4 v[CT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            f[c] = w4_scale<WHOLE>(joined[c], i, left, l);
+            v[c] = w4_codes(p[c], i, l);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            bf16x8 wa[CT];
+#pragma unroll
+            for (int c = 0; c < CT; ++c) wa[c] = w4_values(v[c][q], f[c]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const bf16x8 xb = *reinterpret_cast<const bf16x8*>(x[n] + at + 64 * i + 16 * q);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) acc[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[c], xb, acc[c][n], 0, 0, 0);
+            }
+        }
+    }
+}
+template <int CT, int PIECE, int NT>
+__device__ __forceinline__ void w4_multiply(f32x4 (&acc)[CT][NT], const W4Piece<PIECE> (&p)[CT], const char* const (&x)[NT], int at, int left, const W4Lane& l) {
+    if (left >= PIECE * W4_STEP) w4_multiply_steps<true>(acc, p, x, at, left, l);
+    else w4_multiply_steps<false>(acc, p, x, at, left, l);
+}
+
+// Four classes' biases; zeros without a bias and beyond the shard.
+__device__ __forceinline__ f32x4 w4_bias(const W4Args& a, int cls) {
+    f32x4 b = {0.f, 0.f, 0.f, 0.f};
+    if (a.bias != nullptr)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (cls + e < a.C) b[e] = a.bias[cls + e];
+    return b;
+}
+
+// The logits of four neighbouring classes of 16 NT rows: stored, or held against the best so far.
+template <int NT, bool TOP1>
+__device__ __forceinline__ void w4_finish(const W4Args& a, const f32x4 (&acc)[NT], f32x4 b, int cls, int row0, int rows, int i16, float (&best)[NT],
+                                          int (&best_at)[NT]) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const f32x4 v = acc[n] + b;
+        if constexpr (TOP1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (cls + e < a.C) better_of(best[n], best_at[n], v[e], cls + e);
+        } else {
+            const int r = 16 * n + i16;
+            if (r >= rows) continue;
+            float* z = a.Z + (int64_t)(row0 + r) * a.ldz + cls;
+            if (cls + 4 <= a.C) {
+                *reinterpret_cast<f32x4*>(z) = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (cls + e < a.C) z[e] = v[e];
+            }
+        }
+    }
+}
+
+// The workgroup's candidates of its rows, out of its lanes' and waves'.
+template <int NT, int WAVES>
+__device__ __forceinline__ void w4_report(const W4Args& a, float (&best)[NT], int (&best_at)[NT], int row0, int rows, const W4Lane& l, char* lds) {
     constexpr int R = 16 * NT;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i16 = lane & 15, g = lane >> 4;
+    __syncthreads();                                                           // the features have been read
+    float* sv = reinterpret_cast<float*>(lds);
+    int* sc = reinterpret_cast<int*>(sv + WAVES * R);
+    const int tid = threadIdx.x, wave = tid >> 6;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        better_of(best[n], best_at[n], __shfl_xor(best[n], 16, 64), __shfl_xor(best_at[n], 16, 64));
+        better_of(best[n], best_at[n], __shfl_xor(best[n], 32, 64), __shfl_xor(best_at[n], 32, 64));
+        if (l.g == 0) {
+            sv[wave * R + 16 * n + l.i16] = best[n];
+            sc[wave * R + 16 * n + l.i16] = best_at[n];
+        }
+    }
+    __syncthreads();
+    if (tid < rows) {
+        float v = sv[tid];
+        int at = sc[tid];
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) better_of(v, at, sv[k * R + tid], sc[k * R + tid]);
+        a.part_val[(int64_t)(row0 + tid) * gridDim.x + blockIdx.x] = v;
+        a.part_cls[(int64_t)(row0 + tid) * gridDim.x + blockIdx.x] = at;
+    }
+}
+
+// `chunk` steps of the features are in LDS at a time.
+template <int NT, bool MX, bool TOP1>
+__global__ __launch_bounds__(W4Shape<NT>::THREADS) void w4_product(W4Args a, int chunk, int groups) {
+    typedef W4Shape<NT> S;
+    constexpr int CT = S::CT, PIECE = S::PIECE, R = S::ROWS, WAVES = S::WAVES;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const W4Lane l(tid & 63, a);
+    const int i16 = l.i16, g = l.g;
     const int row0 = blockIdx.y * R;
     const int rows = a.B - row0 < R ? a.B - row0 : R;
-    const int pitch = 2 * chunk + 16;
+    const int pitch = 64 * chunk + 16, plane = (rows * pitch + 255) & ~255;
+    // rows beyond the batch and classes beyond the shard repeat the last one: nothing of them is kept
     const char* x[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) x[n] = lds + (16 * n + i16 < rows ? 16 * n + i16 : rows - 1) * pitch + 256 * g;
+    for (int n = 0; n < NT; ++n) x[n] = lds + g * plane + (16 * n + i16 < rows ? 16 * n + i16 : rows - 1) * pitch;
     float best[NT];
     int best_at[NT];
 #pragma unroll
@@ -81,204 +314,446 @@ __global__ __launch_bounds__(64 * W4_WAVES) void w4_product(W4Args a, int chunk,
         best[n] = -INFINITY;
         best_at[n] = INT_MAX;
     }
+    const bool whole = chunk * W4_STEP >= a.D;                                 // staged once for all groups
 
-  for (int group = blockIdx.x; group < groups; group += gridDim.x) {
-    const int class0 = (group * W4_WAVES + wave) * 16 * CT;
-    // classes beyond the shard and rows beyond the batch repeat the last one: nothing of them is kept
-    const uint8_t* w[CT];
-    const uint8_t* ws[CT];
+    for (int group = blockIdx.x; group < groups; group += gridDim.x) {
+        const int class0 = group * S::CLASSES + wave * 16 * CT;
+        f32x4 acc[CT][NT];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        const int cls = class0 + 16 * c + i16;
-        const int64_t at = cls < a.C ? cls : a.C - 1;
-        w[c] = a.W + at * a.ldw + 64 * g;
-        ws[c] = a.ws + at * a.lds + 4 * g;
-    }
-    f32x4 acc[CT][NT];
+        for (int c = 0; c < CT; ++c)
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int n = 0; n < NT; ++n) acc[c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    for (int k0 = 0; k0 < a.D; k0 += chunk) {
-        const int valid = a.D - k0 < chunk ? a.D - k0 : chunk;                 // a multiple of 64
-        const int wide = (valid + W4_SPAN - 1) / W4_SPAN * W4_SPAN;            // zeros behind: weights that are not there count nothing
-        __syncthreads();                                                       // the chunk before has been read
-        const int units = wide >> 4;                                           // 16 features
-        for (int u = tid; u < rows * units; u += 64 * W4_WAVES) {
-            const int r = u / units, c = u - r * units;
-            u32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-            if (16 * c < valid) {
-                const int64_t row = row0 + r;
-                if constexpr (MX) {
-                    const u32x4 v = *reinterpret_cast<const u32x4*>(a.X + row * a.ldx + k0 + 16 * c);
-                    const float s = scale_of(a.xs[row * a.ldxs + (k0 >> 5) + (c >> 1)], 0);
+        W4Piece<PIECE> even[CT], odd[CT];
+        auto load = [&](W4Piece<PIECE> (&p)[CT], int k) {
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        lo[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e], s, false));
-                        lo[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e], s, true));
-                        hi[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 + e], s, false));
-                        hi[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 + e], s, true));
-                    }
-                } else {
-                    const u32x4* p = reinterpret_cast<const u32x4*>(a.X + row * a.ldx + 2 * k0 + 32 * c);
-                    lo = p[0];
-                    hi = p[1];
-                }
+            for (int c = 0; c < CT; ++c) w4_load(p[c], W4Tile(a, class0 + 16 * c), l, k);
+        };
+        load(even, 0);
+        for (int k0 = 0; k0 < a.D; k0 += chunk * W4_STEP) {
+            if (!whole || group == (int)blockIdx.x) {
+                if (k0 > 0 || group != (int)blockIdx.x) __syncthreads();       // the chunk before has been read
+                const int left = (a.D - k0 + W4_STEP - 1) / W4_STEP;
+                w4_stage<S::THREADS, MX>(a, row0, rows, k0, left < chunk ? left : chunk, lds, pitch, plane);
+                __syncthreads();
             }
-            u32x4* q = reinterpret_cast<u32x4*>(lds + r * pitch + 32 * c);
-            q[0] = lo;
-            q[1] = hi;
+            const int end = k0 + chunk * W4_STEP < a.D ? k0 + chunk * W4_STEP : a.D;
+            for (int k = k0; k < end; k += 2 * PIECE * W4_STEP) {
+                constexpr int SPAN = PIECE * W4_STEP;
+                load(odd, k + SPAN);
+                w4_multiply_steps<false>(acc, even, x, (k - k0) / 2, a.D - k, l);
+                load(even, k + 2 * SPAN);
+                if (k + SPAN < end) w4_multiply_steps<false>(acc, odd, x, (k - k0) / 2 + 64 * PIECE, a.D - k - SPAN, l);
+            }
         }
-        __syncthreads();
-        for (int s = 0; s < valid; s += W4_SPAN) {
-            const int mine = a.D - k0 - s - 128 * g;                           // features from the lane's first on
-            u32x4 v[CT][4];
-            uint32_t sc[CT];
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                const uint8_t* p = w[c] + ((k0 + s) >> 1);
-                const uint8_t* ps = ws[c] + ((k0 + s) >> 5);
-                sc[c] = 0;
-                if (mine > 0) sc[c] = *reinterpret_cast<const uint16_t*>(ps);
-                if (mine > 64) sc[c] |= (uint32_t)*reinterpret_cast<const uint16_t*>(ps + 2) << 16;
+        for (int c = 0; c < CT; ++c)
+            w4_finish<NT, TOP1>(a, acc[c], w4_bias(a, class0 + 16 * c + 4 * g), class0 + 16 * c + 4 * g, row0, rows, i16, best, best_at);
+    }
+    if constexpr (TOP1) w4_report<NT, WAVES>(a, best, best_at, row0, rows, l, lds);
+}
+
+// ---- few rows, many classes --------------------------------------------------------------------------------------------
+// One workgroup to a compute unit holds all features of up to 16 NT rows in LDS.  Its 16 waves walk tiles of 16 classes, each by itself, with
+// no barrier between them: a tile's codes are a stream of pieces of 512 features, RING of them loaded at a time.  With many tiles the waves'
+// loads cover for each other and RING = 1 does: the code is short, and a kernel of a few us pays for every line of it (all kernels start with an
+// empty instruction cache; 8 rows x 512 features x 2000 classes 3.2 us, RING = 2 4.8, 3 6.4).
+constexpr int W4_STREAM_WAVES = 16, W4_STREAM_THREADS = 64 * W4_STREAM_WAVES;
+constexpr int W4_STREAM_PIECE = 4;
+
+template <int NT, int RING, bool MX, bool TOP1>
+__global__ __launch_bounds__(W4_STREAM_THREADS) void w4_stream(W4Args a, int tiles) {
+    constexpr int PIECE = W4_STREAM_PIECE, SPAN = PIECE * W4_STEP;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const W4Lane l(tid & 63, a);
+    const int rows = a.B, steps = (a.D + W4_STEP - 1) / W4_STEP;
+    const int pitch = 64 * steps + 16, plane = (rows * pitch + 255) & ~255;
+    const int stride = gridDim.x * W4_STREAM_WAVES;
+
+    // the piece that is loaded next; behind the last tile nothing is there
+    int tile = wave * gridDim.x + blockIdx.x, k = 0;
+    int now = tile, at = 0;                                                        // the piece that is multiplied
+    W4Piece<PIECE> ring[RING][1];
+    f32x4 bias[RING];                                                              // of the tile that ends with this piece
+    W4Tile aim(a, 16 * tile);
+    const __amdgpu_buffer_rsrc_t biases =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.bias), 0, a.bias != nullptr ? (int)(4u * (uint32_t)a.C) : 0, 0x00020000);
+    auto load = [&](int i) {
+        w4_load(ring[i][0], aim, l, k);
+        k += SPAN;
+        const bool last = k >= a.D;
+        int from = 64 * tile;                                                      // no bias is fetched with the other pieces
+        if (!last) from = -1024;
+        bias[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, 16 * l.g, from, 0));
+        if (last) {
+            k = 0;
+            tile = tile + stride < tiles ? tile + stride : tiles;
+            aim = W4Tile(a, 16 * tile);
+        }
+    };
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[c][i] = u32x4{0, 0, 0, 0};
-                    if (mine > 32 * i) v[c][i] = *reinterpret_cast<const u32x4*>(p + 16 * i);
-                }
+    for (int i = 0; i < RING; ++i) load(i);
+    w4_stage<W4_STREAM_THREADS, MX>(a, 0, rows, 0, steps, lds, pitch, plane);
+    __syncthreads();
+
+    const char* x[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) x[n] = lds + l.g * plane + (16 * n + l.i16 < rows ? 16 * n + l.i16 : rows - 1) * pitch;
+    float best[NT];
+    int best_at[NT];
+    f32x4 acc[1][NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        best[n] = -INFINITY;
+        best_at[n] = INT_MAX;
+        acc[0][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    while (now < tiles) {
+#pragma unroll
+        for (int i = 0; i < RING; ++i) {                                           // pieces behind the last tile are zeros, and their classes beyond the shard
+            w4_multiply<1, PIECE, NT>(acc, ring[i], x, at / 2, a.D - at, l);
+            at += SPAN;
+            if (at >= a.D) {
+                const int cls = 16 * now + 4 * l.g;                                // a lane holds four neighbouring classes of a row
+                w4_finish<NT, TOP1>(a, acc[0], bias[i], cls, 0, rows, l.i16, best, best_at);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[0][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+                at = 0;
+                now = now + stride < tiles ? now + stride : tiles;
             }
+            load(i);
+        }
+    }
+    if constexpr (TOP1) w4_report<NT, W4_STREAM_WAVES>(a, best, best_at, 0, rows, l, lds);
+}
+
+// ---- few rows --------------------------------------------------------------------------------------------------------
+// The waves of a workgroup share out the contraction, so that all codes of its classes are on their way at once, and the waves' partial sums
+// meet in LDS.  One workgroup per group of classes, most of a compute unit's wave slots filled with them: reading alone, W of 100 000 x 2048
+// takes 16.9 us so, 19.9 with a wave for 16 whole rows; 1000 x 4096 2.8 and 6.8.
+//
+// WK = 1 << wk_shift waves along the contraction, wave k the steps S k .. S k + S - 1; the 8 / WK groups of waves take CT tiles of 16 classes
+// each.  Rows go 16 at a time, and P steps of them at a time through LDS, where each wave has a region of its own.
+constexpr int W4_FEW_ROWS = 64;
+constexpr int W4_FEW_WAVES = 8, W4_FEW_THREADS = 64 * W4_FEW_WAVES;
+constexpr int w4_few_piece(int S, int CT, bool MX) { return S >= 2 && S <= 4 && (MX || CT * S == 2) ? 2 : 1; }          // P, as many as the registers hold
+constexpr int w4_few_plane(int P, int rows) { return (rows * (64 * P + 16) + 255) & ~255; }
+constexpr int w4_few_region(int P, int CT, int rows) {
+    const int features = 4 * w4_few_plane(P, rows), sums = rows * (16 * CT + 4) * 4;
+    return features > sums ? features : (sums + 255) & ~255;
+}
+
+template <int S, int CT, bool MX, bool TOP1>
+__global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4Args a, int wk_shift) {
+    constexpr int P = w4_few_piece(S, CT, MX), PITCH = 16 * CT + 4, UNITS = MX ? P * 2 : P * 4;        // 16-byte loads of a lane for a piece of 16 rows
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const W4Lane l(lane, a);
+    const int i16 = l.i16, g = l.g;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int WK = 1 << wk_shift, part = wave >> wk_shift;
+    const int step0 = (wave & (WK - 1)) * S;
+    const int most = a.B < 16 ? a.B : 16;
+    const int plane = w4_few_plane(P, most), region = w4_few_region(P, CT, most);
+    char* mine = lds + wave * region;
+    const int first = (blockIdx.x << (3 - wk_shift)) * 16 * CT;                    // the workgroup's first class
+    // this thread's four neighbouring classes in the sum over the waves, of every (512 / quads)-th row
+    const int quads = (4 * CT) << (3 - wk_shift), c4 = tid & (quads - 1);
+    const int cls = first + 4 * c4;
+
+    const f32x4 bias = w4_bias(a, cls);
+
+    // features [8 u, 8 u + 8) (MX: 16) of a piece and row, as the lane's load j: u + units per row * row = lane + 64 j
+    constexpr int ROW_UNITS = MX ? 8 * P : 16 * P;
+    u32x4 xr[UNITS];
+    uint32_t xs[MX ? UNITS : 1];
+    auto fetch = [&](int n0, int s) {
+        const int rows = a.B - n0 < 16 ? a.B - n0 : 16;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (s + 32 * i >= valid) break;                                // no lane has features there
-                float f[CT];
+        for (int j = 0; j < UNITS; ++j) {
+            const int at = lane + 64 * j, r = at / ROW_UNITS, u = at & (ROW_UNITS - 1);
+            const int k = (step0 + s) * W4_STEP + (MX ? 16 : 8) * u;
+            xr[j] = u32x4{0, 0, 0, 0};
+            if constexpr (MX) xs[j] = 0;
+            if (r < rows && k < a.D) {
+                const int64_t row = n0 + r;
+                xr[j] = *reinterpret_cast<const u32x4*>(a.X + row * a.ldx + (MX ? k : 2 * k));
+                if constexpr (MX) xs[j] = a.xs[row * a.ldxs + (k >> 5)];
+            }
+        }
+    };
+    auto stage = [&](int rows) {
 #pragma unroll
-                for (int c = 0; c < CT; ++c) f[c] = scale_of(sc[c], i);
+        for (int j = 0; j < UNITS; ++j) {
+            const int at = lane + 64 * j, r = at / ROW_UNITS, u = at & (ROW_UNITS - 1);
+            if (r >= rows) continue;
+            if constexpr (MX) {
+                const float f = scale_of(xs[j], 0);
+                u32x4* to = reinterpret_cast<u32x4*>(mine + ((u >> 1) & 3) * plane + r * (64 * P + 16) + (u >> 3) * 64 + (u & 1) * 32);
+                to[0] = w4_features(xr[j][0], xr[j][1], f);
+                to[1] = w4_features(xr[j][2], xr[j][3], f);
+            } else {
+                *reinterpret_cast<u32x4*>(mine + ((u >> 2) & 3) * plane + r * (64 * P + 16) + (u >> 4) * 64 + (u & 3) * 16) = xr[j];
+            }
+        }
+    };
+    const int steps = (a.D + W4_STEP - 1) / W4_STEP;
+    const bool busy = step0 < steps;                                               // waves beyond the contraction only add up
+    if (busy) fetch(0, 0);                                                         // from the cache, and staged while the codes are on their way
+    W4Piece<S> codes[CT];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    bf16x8 wa[CT];
+    for (int c = 0; c < CT; ++c) w4_load(codes[c], W4Tile(a, busy ? first + 16 * (part * CT + c) : a.C), l, step0 * W4_STEP);
+    for (int n0 = 0; n0 < a.B; n0 += 16) {
+        const int rows = a.B - n0 < 16 ? a.B - n0 : 16;
+        f32x4 acc[CT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (busy) {
+            uint32_t joined[CT][W4Piece<S>::HELD];
+            const char* x = mine + g * plane + (i16 < rows ? i16 : rows - 1) * (64 * P + 16);
+#pragma unroll
+            for (int s0 = 0; s0 < S; s0 += P) {
+                stage(rows);
+                if (s0 + P < S) {
+                    fetch(n0, s0 + P);
+                } else if (n0 + 16 < a.B) {
+                    fetch(n0 + 16, 0);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");             // LDS serves a wave's accesses in their order
+                if (s0 == 0)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) w4_join(joined[c], codes[c]);
+#pragma unroll
+                for (int s = s0; s < s0 + P; ++s) {
+                    if (step0 + s >= steps) continue;
+                    float f[CT];
+                    u32x4 v[CT];
 #pragma unroll
                     for (int c = 0; c < CT; ++c) {
-                        const uint32_t codes = v[c][i][q];
-                        u32x4 t;
-                        t[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, f[c], 0));
-                        t[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, f[c], 1));
-                        t[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, f[c], 2));
-                        t[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, f[c], 3));
-                        wa[c] = __builtin_bit_cast(bf16x8, t);
+                        f[c] = w4_scale<false>(joined[c], s, a.D - step0 * W4_STEP, l);
+                        v[c] = w4_codes(codes[c], s, l);
                     }
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const bf16x8 xb = *reinterpret_cast<const bf16x8*>(x[n] + 2 * s + 64 * i + 16 * q);
+                    for (int q = 0; q < 4; ++q) {
+                        const bf16x8 xb = *reinterpret_cast<const bf16x8*>(x + 64 * (s - s0) + 16 * q);
 #pragma unroll
-                        for (int c = 0; c < CT; ++c) acc[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[c], xb, acc[c][n], 0, 0, 0);
+                        for (int c = 0; c < CT; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w4_values(v[c][q], f[c]), xb, acc[c], 0, 0, 0);
                     }
                 }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
         }
-    }
-
-    // a lane holds four neighbouring classes of a row
-    if constexpr (!TOP1) {
+        if (i16 < rows) {
+            float* to = reinterpret_cast<float*>(mine) + i16 * PITCH + 4 * g;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            const int cls = class0 + 16 * c + 4 * g;
-            f32x4 b = {0.f, 0.f, 0.f, 0.f};
-            if (a.bias != nullptr)
+            for (int c = 0; c < CT; ++c) *reinterpret_cast<f32x4*>(to + 16 * c) = acc[c];
+        }
+        wait_counts<NO_VM_WAIT, 0>();
+        raw_barrier();                                                             // loads stay in flight
+        const char* from = lds + ((c4 / (4 * CT)) << wk_shift) * region + 16 * (c4 & (4 * CT - 1));
+        for (int r = tid / quads; r < rows; r += W4_FEW_THREADS / quads) {
+            f32x4 z = *reinterpret_cast<const f32x4*>(from + r * PITCH * 4);
+            for (int k = 1; k < WK; ++k) z += *reinterpret_cast<const f32x4*>(from + k * region + r * PITCH * 4);
+            z += bias;
+            if constexpr (TOP1) {
+                float best = -INFINITY;
+                int at = INT_MAX;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (cls + e < a.C) b[e] = a.bias[cls + e];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int r = 16 * n + i16;
-                if (r >= rows) continue;
-                float* z = a.Z + (int64_t)(row0 + r) * a.ldz + cls;
-                const f32x4 v = acc[c][n] + b;
+                    if (cls + e < a.C) better_of(best, at, z[e], cls + e);
+                for (int m = 1; m < quads; m <<= 1) better_of(best, at, __shfl_xor(best, m, 64), __shfl_xor(at, m, 64));       // a row's lanes are neighbours
+                if (c4 == 0) {
+                    a.part_val[(int64_t)(n0 + r) * gridDim.x + blockIdx.x] = best;
+                    a.part_cls[(int64_t)(n0 + r) * gridDim.x + blockIdx.x] = at;
+                }
+            } else {
+                float* out = a.Z + (int64_t)(n0 + r) * a.ldz + cls;
                 if (cls + 4 <= a.C) {
-                    *reinterpret_cast<f32x4*>(z) = v;
+                    *reinterpret_cast<f32x4*>(out) = z;
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (cls + e < a.C) z[e] = v[e];
+                        if (cls + e < a.C) out[e] = z[e];
                 }
             }
         }
-    } else {
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int cls = class0 + 16 * c + 4 * g + e;
-                    if (cls < a.C) better_of(best[n], best_at[n], acc[c][n][e] + (a.bias != nullptr ? a.bias[cls] : 0.0f), cls);
-                }
+        if (n0 + 16 < a.B) {
+            wait_counts<NO_VM_WAIT, 0>();
+            raw_barrier();                                                         // the sums have been read
+        }
     }
-  }
-    if constexpr (TOP1) {
-        __syncthreads();                                                       // the features have been read
-        float* sv = reinterpret_cast<float*>(lds);
-        int* sc = reinterpret_cast<int*>(sv + W4_WAVES * R);
+}
+
+// The arg-max's candidates of a row, `parts` of them, shard-local classes, one workgroup to a row.
+__global__ __launch_bounds__(256) void w4_merge_top1(const float* __restrict__ val, const int* __restrict__ cls, int parts, int class_offset,
+                                                     float* __restrict__ top_logit, int* __restrict__ top_class) {
+    __shared__ float sv[4];
+    __shared__ int sc[4];
+    const int64_t row = (int64_t)blockIdx.x * parts;
+    float best = -INFINITY;
+    int at = INT_MAX;
+    for (int p = threadIdx.x; p < parts; p += 256) better_of(best, at, val[row + p], cls[row + p]);
+    for (int m = 32; m > 0; m >>= 1) better_of(best, at, __shfl_xor(best, m, 64), __shfl_xor(at, m, 64));
+    if ((threadIdx.x & 63) == 0) {
+        sv[threadIdx.x >> 6] = best;
+        sc[threadIdx.x >> 6] = at;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            better_of(best[n], best_at[n], __shfl_xor(best[n], 16, 64), __shfl_xor(best_at[n], 16, 64));
-            better_of(best[n], best_at[n], __shfl_xor(best[n], 32, 64), __shfl_xor(best_at[n], 32, 64));
-            if (g == 0) {
-                sv[wave * R + 16 * n + i16] = best[n];
-                sc[wave * R + 16 * n + i16] = best_at[n];
-            }
-        }
-        __syncthreads();
-        if (tid < rows) {
-            float v = sv[tid];
-            int at = sc[tid];
-#pragma unroll
-            for (int k = 1; k < W4_WAVES; ++k) better_of(v, at, sv[k * R + tid], sc[k * R + tid]);
-            a.part_val[(int64_t)blockIdx.x * a.B + row0 + tid] = v;
-            a.part_cls[(int64_t)blockIdx.x * a.B + row0 + tid] = at == INT_MAX ? at : at + a.class_offset;
-        }
+        for (int w = 1; w < 4; ++w) better_of(best, at, sv[w], sc[w]);
+        top_logit[blockIdx.x] = best;
+        top_class[blockIdx.x] = at == INT_MAX ? at : at + class_offset;
     }
 }
 
 static inline bool al(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-static int w4_row_tiles(int B) { return B <= 16 ? 1 : B <= 32 ? 2 : 4; }
-static int w4_groups(int C) { return (C + 63) / 64; }                          // of classes that a workgroup takes at a time
-// Workgroups along the classes of the arg-max, each with a candidate for every row; they walk the groups.
+// Rows are cut evenly into blocks of at most eight tiles of 16.
+static int w4_row_tiles(int B) {
+    const int tiles = (B + 15) / 16, blocks = (tiles + 7) / 8;
+    return (tiles + blocks - 1) / blocks;
+}
+
+// How a call is run.  us of the launch, fp32 logits of bf16 features, codes not in any cache (one MI355X):
+//   rows x features x classes    w4_stream RING 1, 2    w4_few       w4_product
+//    1 x 2048 x 100000           24.0  24.9             29           26
+//   16 x 2048 x 100000           27.0  27.2             31           39
+//   32 x 2048 x 100000           31.4  33.9             47           57
+//    1 x  512 x 100000            8.2  10.3             10.7          9.5
+//    1 x 2048 x 12500             8.2   7.6              7.0          7.6
+//   32 x 2048 x 12500            12.2  11.3             11.2         15.9
+//   64 x 2048 x 12500                                   16.9         30.9
+//   64 x 2048 x 100000                                  75           62
+//    1 x 8192 x 12500            24.5  17.0             28           19.6
+//    1 x 4096 x 4000             10.3   8.9              5.4
+//    1 x 4096 x 1000             10.1   8.6              4.8          8.9
+//    8 x  512 x 2000              3.2   4.8              3.9
+// A wave of w4_stream takes whole rows of 16 classes: with few of them most waves have nothing to do, and w4_few shares the rows out.  Its second
+// barrier-bound half costs some 3 us, so short rows and many classes stay on w4_stream.
+enum W4Way { W4_STREAM, W4_FEW, W4_PRODUCT };
+struct W4Plan {
+    W4Way way;
+    int groups;                              // workgroups along the classes
+    int ring;                                // w4_stream
+    int S, CT, wk_shift;                     // w4_few
+};
+constexpr size_t W4_STREAM_LDS = 160 * 1024;
+static size_t w4_stream_lds(int B, int D) {
+    const size_t steps = (D + W4_STEP - 1) / W4_STEP;
+    return 4 * (((size_t)B * (64 * steps + 16) + 255) & ~(size_t)255);
+}
+static W4Plan w4_plan(int B, int D, int C) {
+    W4Plan p = {W4_PRODUCT, 0, 1, 1, 1, 3};
+    const int64_t tiles = ((int64_t)C + 15) / 16;
+    const int steps = (D + W4_STEP - 1) / W4_STEP;
+    const bool fits = B <= 32 && w4_stream_lds(B, D) <= W4_STREAM_LDS;
+    const int64_t most = steps <= 32 ? 1024 : 512;                                 // tiles up to which rows are shared out
+    if (B <= W4_FEW_ROWS && steps <= 8 * W4_FEW_WAVES && (fits ? steps >= 8 && tiles <= most : tiles * ((B + 15) / 16) <= 4 * most)) {
+        p.way = W4_FEW;
+        while (W4_FEW_WAVES * p.S < steps) p.S *= 2;
+        while (p.wk_shift > 0 && (1 << (p.wk_shift - 1)) * p.S >= steps) --p.wk_shift;
+        // as many classes to a workgroup as the registers hold, while there are workgroups for most compute units
+        p.CT = p.S == 1 ? (p.wk_shift == 0 ? 2 : 4) : p.S == 2 ? 4 : p.S == 4 ? 2 : 1;
+        if (p.S > 1 && tiles < 192 * p.CT) p.CT = 1;
+        const int64_t at_once = (int64_t)p.CT << (3 - p.wk_shift);
+        p.groups = (int)((tiles + at_once - 1) / at_once);
+    } else if (fits) {
+        p.way = W4_STREAM;
+        p.groups = tiles < 256 ? (int)tiles : 256;
+        p.ring = steps > 32 && tiles <= 1024 ? 2 : 1;
+    }
+    return p;
+}
+
+static int w4_classes(int B) { return w4_row_tiles(B) <= 2 ? W4Shape<1>::CLASSES : W4Shape<8>::CLASSES; }
+static int w4_groups(int B, int C) { return (int)(((int64_t)C + w4_classes(B) - 1) / w4_classes(B)); }        // of classes that a workgroup takes at a time
+// Workgroups along the classes of the arg-max on w4_product, each with a candidate for every row; they walk the groups.
 constexpr int W4_MAX_PARTS = 4096;
-static int w4_parts(int C) { return w4_groups(C) < W4_MAX_PARTS ? w4_groups(C) : W4_MAX_PARTS; }
+static int w4_parts(int B, int D, int C) {
+    const W4Plan p = w4_plan(B, D, C);
+    return p.way != W4_PRODUCT ? p.groups : w4_groups(B, C) < W4_MAX_PARTS ? w4_groups(B, C) : W4_MAX_PARTS;
+}
+
+template <int S, int CT, bool MX, bool TOP1>
+static void launch_w4_few(const W4Args& a, const W4Plan& f, hipStream_t s) {
+    const size_t bytes = (size_t)W4_FEW_WAVES * w4_few_region(w4_few_piece(S, CT, MX), CT, a.B < 16 ? a.B : 16);
+    hipLaunchKernelGGL((w4_few<S, CT, MX, TOP1>), dim3(f.groups), dim3(W4_FEW_THREADS), bytes, s, a, f.wk_shift);
+}
+
+template <bool MX, bool TOP1>
+static void launch_w4_steps(const W4Args& a, const W4Plan& f, hipStream_t s) {
+    switch (f.S * 8 + f.CT) {
+        case 1 * 8 + 2: return launch_w4_few<1, 2, MX, TOP1>(a, f, s);
+        case 1 * 8 + 4: return launch_w4_few<1, 4, MX, TOP1>(a, f, s);
+        case 2 * 8 + 1: return launch_w4_few<2, 1, MX, TOP1>(a, f, s);
+        case 2 * 8 + 4: return launch_w4_few<2, 4, MX, TOP1>(a, f, s);
+        case 4 * 8 + 1: return launch_w4_few<4, 1, MX, TOP1>(a, f, s);
+        case 4 * 8 + 2: return launch_w4_few<4, 2, MX, TOP1>(a, f, s);
+        default: return launch_w4_few<8, 1, MX, TOP1>(a, f, s);
+    }
+}
 
 template <int NT, bool MX, bool TOP1>
 static void launch_w4_tiles(const W4Args& a, hipStream_t s) {
-    const int most = NT == 1 ? 1536 : NT == 2 ? 512 : 512;
-    const int chunk = a.D < most ? (a.D + W4_SPAN - 1) / W4_SPAN * W4_SPAN : most;
-    const int rows = a.B < 16 * NT ? a.B : 16 * NT;
-    size_t bytes = (size_t)rows * (2 * chunk + 16);
-    const size_t least = TOP1 ? (size_t)W4_WAVES * 16 * NT * 8 : 0;
+    typedef W4Shape<NT> S;
+    const int rows = a.B < S::ROWS ? a.B : S::ROWS;
+    const int steps = (a.D + W4_STEP - 1) / W4_STEP;
+    // all of them, or whole pairs of pieces: the kernel takes two in turn and a chunk has to hold one pair at least
+    static_assert(w4_chunk(S::ROWS) >= 2 * S::PIECE, "");
+    int chunk = w4_chunk(rows);
+    chunk = chunk >= steps ? steps : chunk / (2 * S::PIECE) * (2 * S::PIECE);
+    const int plane = (rows * (64 * chunk + 16) + 255) & ~255;
+    size_t bytes = 4 * (size_t)plane;
+    const size_t least = TOP1 ? (size_t)S::WAVES * S::ROWS * 8 : 0;
     if (bytes < least) bytes = least;
-    hipLaunchKernelGGL((w4_product<NT, 1, MX, TOP1>), dim3(TOP1 ? w4_parts(a.C) : w4_groups(a.C), (a.B + 16 * NT - 1) / (16 * NT)),
-                       dim3(64 * W4_WAVES), bytes, s, a, chunk, w4_groups(a.C));
+    const int groups = w4_groups(a.B, a.C);
+    hipLaunchKernelGGL((w4_product<NT, MX, TOP1>), dim3(TOP1 ? w4_parts(a.B, a.D, a.C) : groups, (a.B + S::ROWS - 1) / S::ROWS), dim3(S::THREADS), bytes, s, a,
+                       chunk, groups);
+}
+
+template <int NT, int RING, bool MX, bool TOP1>
+static void launch_w4_stream(const W4Args& a, const W4Plan& p, hipStream_t s) {
+    size_t bytes = w4_stream_lds(a.B, a.D);
+    const size_t least = TOP1 ? (size_t)W4_STREAM_WAVES * 16 * NT * 8 : 0;
+    if (bytes < least) bytes = least;
+    hipLaunchKernelGGL((w4_stream<NT, RING, MX, TOP1>), dim3(p.groups), dim3(W4_STREAM_THREADS), bytes, s, a, (int)(((int64_t)a.C + 15) / 16));
+}
+
+template <bool MX, bool TOP1>
+static void launch_w4_type(const W4Args& a, hipStream_t s) {
+    const W4Plan p = w4_plan(a.B, a.D, a.C);
+    if (p.way == W4_FEW) return launch_w4_steps<MX, TOP1>(a, p, s);
+    if (p.way == W4_STREAM) {
+        if (a.B > 16) return launch_w4_stream<2, 1, MX, TOP1>(a, p, s);
+        return p.ring == 1 ? launch_w4_stream<1, 1, MX, TOP1>(a, p, s) : launch_w4_stream<1, 2, MX, TOP1>(a, p, s);
+    }
+    switch (w4_row_tiles(a.B)) {
+        case 1: return launch_w4_tiles<1, MX, TOP1>(a, s);
+        case 2: return launch_w4_tiles<2, MX, TOP1>(a, s);
+        case 3: return launch_w4_tiles<3, MX, TOP1>(a, s);
+        case 4: return launch_w4_tiles<4, MX, TOP1>(a, s);
+        case 5: return launch_w4_tiles<5, MX, TOP1>(a, s);
+        case 6: return launch_w4_tiles<6, MX, TOP1>(a, s);
+        case 7: return launch_w4_tiles<7, MX, TOP1>(a, s);
+        default: return launch_w4_tiles<8, MX, TOP1>(a, s);
+    }
 }
 
 template <bool TOP1>
 static void launch_w4(const W4Args& a, hipStream_t s) {
-    const int nt = w4_row_tiles(a.B);
-    if (a.xs != nullptr) {
-        if (nt == 1) launch_w4_tiles<1, true, TOP1>(a, s);
-        else if (nt == 2) launch_w4_tiles<2, true, TOP1>(a, s);
-        else launch_w4_tiles<4, true, TOP1>(a, s);
-    } else {
-        if (nt == 1) launch_w4_tiles<1, false, TOP1>(a, s);
-        else if (nt == 2) launch_w4_tiles<2, false, TOP1>(a, s);
-        else launch_w4_tiles<4, false, TOP1>(a, s);
-    }
+    if (a.xs != nullptr) launch_w4_type<true, TOP1>(a, s);
+    else launch_w4_type<false, TOP1>(a, s);
 }
 
 static int check_w4(const void* X, int64_t ldx, const void* X_scales, int64_t ldxs, const void* W4, int64_t ldw4, const void* W_scales,
                     int64_t lds, const float* b_shard, int32_t B, int32_t D, int32_t C_shard) {
     if (!X || !W4 || !W_scales) return WS_ERR_NULL;
     if (B <= 0 || D <= 0 || C_shard <= 0 || D % 64 || B > W4_MAX_ROWS) return WS_ERR_SHAPE;
-    if (C_shard > INT32_MAX - 4096) return WS_ERR_RANGE;                       // class ids of a whole last group are counted in 31 bits
+    if (ldw4 > W4_MAX_PITCH || lds > W4_MAX_PITCH) return WS_ERR_SHAPE;
+    if (C_shard > INT32_MAX - 65536) return WS_ERR_RANGE;                       // class ids of a whole last group are counted in 31 bits
     if (ldx < D || (X_scales && ldxs < D / MX_GROUP) || ldw4 < D / 2 || lds < D / MX_GROUP) return WS_ERR_SHAPE;
     if (!al(X, 16) || ldx % (X_scales ? 16 : 8) || !al(W4, 16) || ldw4 % 16 || !al(W_scales, 2) || lds % 2) return WS_ERR_ALIGN;
     if ((X_scales && (!al(X_scales, 2) || ldxs % 2)) || (b_shard && !al(b_shard, 4))) return WS_ERR_ALIGN;
@@ -328,8 +803,12 @@ int ws_split_fc_w4_logits(const void* X, int64_t ldx, const void* X_scales, int6
     return hipGetLastError() == hipSuccess ? WS_OK : WS_ERR_HIP;
 }
 
+// Whatever the number of features: w4_few has at most a workgroup for 16 classes, and 2048 of them for up to 64 rows; w4_stream has fewer.
 size_t ws_w4_top1_workspace_bytes(int32_t B, int32_t C_shard) {
-    return B > 0 && C_shard > 0 ? (size_t)w4_parts(C_shard) * B * 8 : 0;
+    if (B <= 0 || C_shard <= 0 || B > W4_MAX_ROWS) return 0;
+    const int64_t tiles = ((int64_t)C_shard + 15) / 16, groups = w4_groups(B, C_shard), many = groups < W4_MAX_PARTS ? groups : W4_MAX_PARTS;
+    const int64_t few = B > W4_FEW_ROWS ? 0 : tiles < W4_MAX_PARTS ? tiles : W4_MAX_PARTS;
+    return (size_t)(few > many ? few : many) * B * 8;
 }
 
 int ws_split_fc_w4_top1(const void* X, int64_t ldx, const void* X_scales, int64_t ldxs, const void* W4, int64_t ldw4, const void* W_scales,
@@ -343,13 +822,13 @@ int ws_split_fc_w4_top1(const void* X, int64_t ldx, const void* X_scales, int64_
     if (!workspace || workspace_bytes < ws_w4_top1_workspace_bytes(B, C_shard)) return WS_ERR_WORKSPACE;
     if (!al(workspace, 16)) return WS_ERR_ALIGN;
     W4Args a = w4_args(X, ldx, X_scales, ldxs, W4, ldw4, W_scales, lds, b_shard, B, D, C_shard);
-    const int parts = w4_parts(C_shard);
+    const int parts = w4_parts(B, D, C_shard);
     a.part_val = static_cast<float*>(workspace);
     a.part_cls = reinterpret_cast<int*>(a.part_val + (int64_t)parts * B);
-    a.class_offset = class_offset;
-    launch_w4<true>(a, static_cast<hipStream_t>(stream));
-    if (hipGetLastError() != hipSuccess) return WS_ERR_HIP;
-    return ws_combine_top1(a.part_val, a.part_cls, parts, B, B, top_logit, top_class, stream);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    launch_w4<true>(a, s);
+    hipLaunchKernelGGL(w4_merge_top1, dim3(B), dim3(256), 0, s, a.part_val, a.part_cls, parts, class_offset, top_logit, top_class);
+    return hipGetLastError() == hipSuccess ? WS_OK : WS_ERR_HIP;
 }
 
 }  // extern "C"
