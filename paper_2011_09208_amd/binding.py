@@ -8,6 +8,7 @@ library has not been built, importing this module raises.
 import array
 import ctypes
 import os
+from operator import attrgetter
 
 import torch
 
@@ -350,51 +351,58 @@ def bridge_fusable(gather_dim, src_extents, partition_dim, dst_extents):
     return bool(ok.value)
 
 
-def _pitch(t, rows, cols, elem_bytes):
-    """Row pitch of a [rows, cols] device tensor whose rows are contiguous; None for no tensor."""
+_BF16, _FP32, _I32, _F64 = torch.bfloat16, torch.float32, torch.int32, torch.float64
+_STREAM_TYPES = {_BF16: 2, _FP32: 4}
+_BYTE_TYPES = (torch.uint8, torch.float8_e4m3fn)
+
+
+def _matrix(t, shape, dtype):
+    """(address, row pitch) of a device tensor of this shape whose rows are contiguous; (None, 0) for no tensor."""
     if t is None:
-        return 0
-    shape = t.shape
-    assert len(shape) == 2 and shape[0] == rows and shape[1] == cols and t.element_size() == elem_bytes and t.is_cuda
+        return None, 0
+    assert t.dtype is dtype and t.shape == shape and t.is_cuda
     ld, unit = t.stride()
-    assert unit == 1 or cols == 1
-    return ld if rows > 1 else max(ld, cols)
+    if unit != 1 or ld < shape[1]:                         # a single row or column may have any stride
+        assert (unit == 1 or shape[1] == 1) and (ld >= shape[1] or shape[0] == 1)
+        ld = max(ld, shape[1])
+    return t.data_ptr(), ld
+
+
+def _bytes_matrix(t, shape):
+    """_matrix of 8-bit values of either type."""
+    return _matrix(t, shape, _BYTE_TYPES[1] if t.dtype is _BYTE_TYPES[1] else _BYTE_TYPES[0])
 
 
 def _vector(t, n, dtype):
-    assert t is None or (t.shape == (n,) and t.dtype == dtype and t.is_contiguous() and t.is_cuda)
-    return None if t is None else t.data_ptr()
+    if t is None:
+        return None
+    assert t.dtype is dtype and t.shape == (n,) and t.is_contiguous() and t.is_cuda
+    return t.data_ptr()
 
 
-_STREAM_TYPES = {torch.bfloat16: 2, torch.float32: 4}
-
-
-def _stream_bytes(*tensors):
-    """Bytes of the residual stream's type: the one that the given tensors (or None) share, bf16 if there is none."""
-    types = {t.dtype for t in tensors if t is not None}
-    assert len(types) <= 1
-    return _STREAM_TYPES[types.pop()] if types else 2
+def _stream_type(a, b):
+    """Type of the residual stream: of the first tensor that is given, bf16 if there is none."""
+    return a.dtype if a is not None else b.dtype if b is not None else _BF16
 
 
 def rms_norm_fwd(x, residual, gamma, eps, h, y, rstd):
     """h = residual + x, y = h * rstd * gamma.  x, y bf16 [B, D]; residual, h bf16 or fp32 [B, D] or None; gamma fp32 [D];
     rstd fp32 [B] or None.  h may be residual itself."""
-    B, D = x.shape
-    es = _stream_bytes(residual, h)
-    assert x.dtype == torch.bfloat16 and y.dtype == torch.bfloat16
-    _check(lib.ws_rms_norm_fwd(x.data_ptr(), _pitch(x, B, D, 2), _ptr(residual), _pitch(residual, B, D, es), es, _vector(gamma, D, torch.float32),
-                               eps, B, D, _ptr(h), _pitch(h, B, D, es), y.data_ptr(), _pitch(y, B, D, 2), _vector(rstd, B, torch.float32),
-                               _stream()))
+    shape = x.shape
+    B, D = shape
+    kind = _stream_type(residual, h)
+    _check(lib.ws_rms_norm_fwd(*_matrix(x, shape, _BF16), *_matrix(residual, shape, kind), _STREAM_TYPES[kind], _vector(gamma, D, _FP32),
+                               eps, B, D, *_matrix(h, shape, kind), *_matrix(y, shape, _BF16), _vector(rstd, B, _FP32), _stream()))
 
 
 def rms_norm_fwd_mx8(x, residual, gamma, eps, h, y, y_scales, rstd):
     """rms_norm_fwd with y in 8 bits: y uint8 or float8_e4m3fn [B, D], y_scales uint8 [B, D / 32]."""
-    B, D = x.shape
-    es = _stream_bytes(residual, h)
-    assert x.dtype == torch.bfloat16
-    _check(lib.ws_rms_norm_fwd_mx8(x.data_ptr(), _pitch(x, B, D, 2), _ptr(residual), _pitch(residual, B, D, es), es,
-                                   _vector(gamma, D, torch.float32), eps, B, D, _ptr(h), _pitch(h, B, D, es), y.data_ptr(), _pitch(y, B, D, 1),
-                                   y_scales.data_ptr(), _pitch(y_scales, B, D // 32, 1), _vector(rstd, B, torch.float32), _stream()))
+    shape = x.shape
+    B, D = shape
+    kind = _stream_type(residual, h)
+    _check(lib.ws_rms_norm_fwd_mx8(*_matrix(x, shape, _BF16), *_matrix(residual, shape, kind), _STREAM_TYPES[kind], _vector(gamma, D, _FP32),
+                                   eps, B, D, *_matrix(h, shape, kind), *_bytes_matrix(y, shape), *_matrix(y_scales, (B, D // 32), torch.uint8),
+                                   _vector(rstd, B, _FP32), _stream()))
 
 
 def rms_norm_bwd_workspace_bytes(B, D):
@@ -404,36 +412,35 @@ def rms_norm_bwd_workspace_bytes(B, D):
 def rms_norm_bwd(dY, h, dres, gamma, rstd, dh, dgamma, workspace):
     """dY fp32 [B, D]; h, dh and dres (or None) bf16 or fp32 [B, D]; gamma fp32 [D]; rstd fp32 [B]; dgamma fp32 [D], or None: then
     workspace may be None, else it has rms_norm_bwd_workspace_bytes.  dh may be dres itself."""
-    B, D = dY.shape
-    es = _stream_bytes(h, dres, dh)
-    _check(lib.ws_rms_norm_bwd(dY.data_ptr(), _pitch(dY, B, D, 4), h.data_ptr(), _pitch(h, B, D, es), _ptr(dres), _pitch(dres, B, D, es), es,
-                               _vector(gamma, D, torch.float32), _vector(rstd, B, torch.float32), B, D, dh.data_ptr(), _pitch(dh, B, D, es),
-                               _vector(dgamma, D, torch.float32), _ptr(workspace),
-                               0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+    shape = dY.shape
+    B, D = shape
+    kind = h.dtype
+    _check(lib.ws_rms_norm_bwd(*_matrix(dY, shape, _FP32), *_matrix(h, shape, kind), *_matrix(dres, shape, kind), _STREAM_TYPES[kind],
+                               _vector(gamma, D, _FP32), _vector(rstd, B, _FP32), B, D, *_matrix(dh, shape, kind), _vector(dgamma, D, _FP32),
+                               _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
 
 
 def quantize_mx4(W, W4, W_scales):
     """W bf16 [C, D] -> W4 uint8 [C, D / 2] (two codes to a byte, the first in the low bits), W_scales uint8 [C, D / 32]."""
     C, D = W.shape
-    assert W.dtype == torch.bfloat16
-    _check(lib.ws_quantize_mx4(W.data_ptr(), _pitch(W, C, D, 2), C, D, W4.data_ptr(), _pitch(W4, C, D // 2, 1), W_scales.data_ptr(),
-                               _pitch(W_scales, C, D // 32, 1), _stream()))
+    _check(lib.ws_quantize_mx4(*_matrix(W, W.shape, _BF16), C, D, *_matrix(W4, (C, D // 2), torch.uint8),
+                               *_matrix(W_scales, (C, D // 32), torch.uint8), _stream()))
 
 
 def _w4_args(X, X_scales, W4, W_scales, b_shard):
-    B, D = X.shape
+    shape = X.shape
+    B, D = shape
     C = W4.shape[0]
-    assert X.dtype == torch.bfloat16 or X_scales is not None
-    return (X.data_ptr(), _pitch(X, B, D, 2 if X_scales is None else 1), _ptr(X_scales), _pitch(X_scales, B, D // 32, 1), W4.data_ptr(),
-            _pitch(W4, C, D // 2, 1), W_scales.data_ptr(), _pitch(W_scales, C, D // 32, 1), _vector(b_shard, C, torch.float32), B, D, C)
+    x = _matrix(X, shape, _BF16) if X_scales is None else _bytes_matrix(X, shape)
+    return (*x, *_matrix(X_scales, (B, D // 32), torch.uint8), *_matrix(W4, (C, D // 2), torch.uint8),
+            *_matrix(W_scales, (C, D // 32), torch.uint8), _vector(b_shard, C, _FP32), B, D, C)
 
 
 def split_fc_w4_logits(X, X_scales, W4, W_scales, b_shard, Z):
     """Z fp32 [B, C_shard] (row pitch a multiple of 4) <- X . W^T + b.  X bf16 [B, D] with X_scales None, or uint8 / float8_e4m3fn with
     X_scales uint8 [B, D / 32]; W4, W_scales as quantize_mx4 leaves them; b_shard fp32 [C_shard] or None."""
-    assert Z.dtype == torch.float32
     a = _w4_args(X, X_scales, W4, W_scales, b_shard)
-    _check(lib.ws_split_fc_w4_logits(*a, Z.data_ptr(), _pitch(Z, a[9], a[11], 4), _stream()))
+    _check(lib.ws_split_fc_w4_logits(*a, *_matrix(Z, (a[9], a[11]), _FP32), _stream()))
 
 
 def w4_top1_workspace_bytes(B, C_shard):
@@ -443,44 +450,45 @@ def w4_top1_workspace_bytes(B, C_shard):
 def split_fc_w4_top1(X, X_scales, W4, W_scales, b_shard, class_offset, top_logit, top_class, workspace):
     """top_logit fp32 [B], top_class int32 [B] <- the shard's best class per row; inputs as split_fc_w4_logits."""
     a = _w4_args(X, X_scales, W4, W_scales, b_shard)
-    _check(lib.ws_split_fc_w4_top1(*a, int(class_offset), _vector(top_logit, a[9], torch.float32), _vector(top_class, a[9], torch.int32),
+    _check(lib.ws_split_fc_w4_top1(*a, int(class_offset), _vector(top_logit, a[9], _FP32), _vector(top_class, a[9], _I32),
                                    workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
 
 
-def _address(values, code="q"):
-    """(address, owner) of the values as a C array; the owner has to outlive the call."""
-    a = array.array(code, values)
-    return a.buffer_info()[0], a
+_ONES = array.array("q", [1]) * 4096
 
 
 class grad_table:
     """The tables that grad_sumsq, grad_clip and grad_clip_sgd take, of bf16 or fp32 device tensors that are contiguous, or
     matrices with contiguous rows.  It holds addresses: build it again when tensors move."""
 
-    def __init__(self, tensors):
-        tensors = list(tensors)
-        self.n = len(tensors)
-        elem_bytes = [_STREAM_TYPES[t.dtype] for t in tensors]
-        rows, cols, lds = [], [], []
-        for t in tensors:
-            if t.dim() == 2:
-                (r, c), (ld, unit) = t.shape, t.stride()
-                assert unit == 1 or c <= 1
+    def __init__(self, tensors, by_rows=False):
+        self.tensors = tensors = list(tensors)
+        self.n = n = len(tensors)
+        T = torch.Tensor
+        elem_bytes = array.array("i", map(_STREAM_TYPES.__getitem__, map(attrgetter("dtype"), tensors)))
+        assert all(map(attrgetter("is_cuda"), tensors))
+        if not by_rows and n <= len(_ONES) and all(map(T.is_contiguous, tensors)):       # each one long row
+            rows = _ONES
+            lds = cols = array.array("q", map(T.numel, tensors))
+        else:
+            rows, cols, lds = [array.array("q") for _ in range(3)]
+            for t in tensors:
+                if t.dim() == 2:
+                    (r, c), (ld, unit) = t.shape, t.stride()
+                    assert unit == 1 or c <= 1
+                else:
+                    assert t.is_contiguous()
+                    r, c, ld = 1, t.numel(), 0
                 rows.append(r)
                 cols.append(c)
                 lds.append(ld if r > 1 else c)
-            else:
-                assert t.is_contiguous()
-                n = t.numel()
-                rows.append(1)
-                cols.append(n)
-                lds.append(n)
-        assert all(t.is_cuda for t in tensors)
-        self.extents = (rows, cols)
-        (self.data, a), (self.rows, b), (self.cols, c), (self.lds, d), (self.bytes, e) = (
-            _address([t.data_ptr() for t in tensors]), _address(rows), _address(cols), _address(lds),
-            _address(elem_bytes, "i"))
-        self._owners = (a, b, c, d, e)
+        data = array.array("q", map(T.data_ptr, tensors))
+        self._arrays = (data, rows, cols, lds, elem_bytes)                   # they own what the addresses point at
+        self.data, self.rows, self.cols, self.lds, self.bytes = [a.buffer_info()[0] for a in self._arrays]
+
+    @property
+    def extents(self):
+        return self._arrays[1][:self.n], self._arrays[2]
 
 
 def _table(tensors):
@@ -502,7 +510,7 @@ def grad_clip(grads, sumsq, max_norm, norm=None):
     """Scales the gradients in place by min(1, max_norm / norm), norm = sqrt(sum of sumsq fp64 [S]); norm fp32 [1] or None."""
     g = _table(grads)
     S = sumsq.numel()
-    _check(lib.ws_grad_clip(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, torch.float64), S, float(max_norm),
+    _check(lib.ws_grad_clip(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, _F64), S, float(max_norm),
                             _vector(norm, 1, torch.float32), _stream()))
 
 
@@ -510,7 +518,9 @@ def grad_clip_sgd(params, grads, sumsq, max_norm, lr, norm=None):
     """params[i] <- params[i] - lr * k * grads[i] with grad_clip's factor k; the gradients are left as they are."""
     p, g = _table(params), _table(grads)
     S = sumsq.numel()
-    assert p.extents == g.extents
+    if p.extents != g.extents:                             # one of a pair has a pitch: both are described by their rows
+        p, g = grad_table(p.tensors, True), grad_table(g.tensors, True)
+        assert p.extents == g.extents
     _check(lib.ws_grad_clip_sgd(p.data, p.lds, p.bytes, g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, torch.float64), S,
                                 float(max_norm), float(lr), _vector(norm, 1, torch.float32), _stream()))
 

@@ -175,12 +175,16 @@ struct NormBackArgs {
 };
 
 // A workgroup walks rows blockIdx.x * ROWS + .., gridDim.x * ROWS apart, and keeps its share of dgamma in registers: a thread's
-// columns are the same in every row.
+// columns are the same in every row.  Where a wave takes a row, eight waves add theirs up: every share costs a write and a read of D floats
+// (1024 x 2048 with four waves: 11.0 us).
+constexpr int NORM_BACK_WAVES = 8;
+constexpr int norm_back_threads(int T) { return T > 64 ? T : 64 * NORM_BACK_WAVES; }
+
 template <int T, int NV, bool FP32>
-__global__ __launch_bounds__(T > 256 ? T : 256) void rms_norm_bwd(NormBackArgs a) {
-    constexpr int ROWS = T > 256 ? 1 : 256 / T;
+__global__ __launch_bounds__(norm_back_threads(T)) void rms_norm_bwd(NormBackArgs a) {
+    constexpr int ROWS = T > 64 ? 1 : NORM_BACK_WAVES;
     __shared__ float part[2][T / 64];
-    __shared__ __attribute__((aligned(16))) float meet[T == 64 ? 3 * 64 * NV * 8 : 1];
+    __shared__ __attribute__((aligned(16))) float meet[T == 64 ? ROWS / 2 * 64 * NV * 8 : 1];
     const int t = threadIdx.x % T, r = threadIdx.x / T;
     const int n = a.D >> 3;
     f32x8 sum[NV];
@@ -233,23 +237,25 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void rms_norm_bwd(NormBackArgs a
         }
     }
     if (a.parts == nullptr) return;
-    if constexpr (T == 64) {             // the four waves' shares, in their order
-        if (r > 0)
+    if constexpr (T == 64) {             // the waves' shares in pairs, pairs of pairs, ..
 #pragma unroll
-            for (int k = 0; k < NV; ++k) store8(meet + ((r - 1) * NV + k) * 512 + 8 * t, sum[k]);
-        __syncthreads();
-        if (r > 0) return;
+        for (int half = ROWS / 2; half > 0; half >>= 1) {
+            if (half < ROWS / 2) __syncthreads();
+            if (r >= half && r < 2 * half)
 #pragma unroll
-        for (int w = 0; w < 3; ++w)
+                for (int k = 0; k < NV; ++k) store8(meet + ((r - half) * NV + k) * 512 + 8 * t, sum[k]);
+            __syncthreads();
+            if (r < half)
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                f32x8 o;
-                load8(meet + (w * NV + k) * 512 + 8 * t, o);
+                for (int k = 0; k < NV; ++k) {
+                    f32x8 o;
+                    load8(meet + (r * NV + k) * 512 + 8 * t, o);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[k][e] += o[e];
-            }
+                    for (int e = 0; e < 8; ++e) sum[k][e] += o[e];
+                }
+        }
     }
-    if (T > 64 && r > 0) return;
+    if (r > 0) return;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int c = t + k * T;
@@ -257,28 +263,30 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void rms_norm_bwd(NormBackArgs a
     }
 }
 
-// dgamma[d] = sum of the workgroups' shares, 32 columns to a workgroup: thread (q, c) sums shares q, q + 32, .., then the 32 sums
-// of a column in their order.
-__global__ __launch_bounds__(1024) void rms_norm_dgamma(const float* __restrict__ parts, int n, int D, float* __restrict__ dgamma) {
-    __shared__ float meet[32][33];
-    const int c = threadIdx.x & 31, q = threadIdx.x >> 5;
-    const int d = blockIdx.x * 32 + c;
-    float s = 0.0f;
-    for (int p = q; p < n; p += 32) s += parts[(int64_t)p * D + d];
-    meet[q][c] = s;
+// dgamma[d] = sum of the workgroups' shares, 32 columns to a workgroup: thread (q, c) sums four columns of shares q, q + 32, .., then the 32 sums
+// of a column are added in their order.
+__global__ __launch_bounds__(256) void rms_norm_dgamma(const float* __restrict__ parts, int n, int D, float* __restrict__ dgamma) {
+    __shared__ float meet[32][36];
+    const int c = threadIdx.x & 7, q = threadIdx.x >> 3;
+    const f32x4* from = reinterpret_cast<const f32x4*>(parts + blockIdx.x * 32 + 4 * c);
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int p = q; p < n; p += 32) s += from[(int64_t)p * (D / 4)];
+    *reinterpret_cast<f32x4*>(&meet[q][4 * c]) = s;
     __syncthreads();
-    if (q == 0) {
+    if (threadIdx.x < 32) {
+        float v = meet[0][threadIdx.x];
 #pragma unroll
-        for (int w = 1; w < 32; ++w) s += meet[w][c];
-        dgamma[d] = s;
+        for (int w = 1; w < 32; ++w) v += meet[w][threadIdx.x];
+        dgamma[blockIdx.x * 32 + threadIdx.x] = v;
     }
 }
 
 // Workgroups of the backward call: each leaves a share of dgamma that has to be written and read again.
 static int norm_back_groups(int B, int D) {
-    const int rows = D <= 2048 ? 4 : 1;
+    const int rows = D <= 2048 ? NORM_BACK_WAVES : 1, most = D <= 2048 ? 256 : 512;
     const int groups = (B + rows - 1) / rows;
-    return groups < 512 ? groups : 512;
+    return groups < most ? groups : most;
 }
 
 static inline bool al(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -309,9 +317,9 @@ static void launch_norm(const NormArgs& a, hipStream_t s) {
 
 template <bool FP32>
 static void launch_norm_back(const NormBackArgs& a, int groups, hipStream_t s) {
-    if (a.D <= 512) hipLaunchKernelGGL((rms_norm_bwd<64, 1, FP32>), dim3(groups), dim3(256), 0, s, a);
-    else if (a.D <= 1024) hipLaunchKernelGGL((rms_norm_bwd<64, 2, FP32>), dim3(groups), dim3(256), 0, s, a);
-    else if (a.D <= 2048) hipLaunchKernelGGL((rms_norm_bwd<64, 4, FP32>), dim3(groups), dim3(256), 0, s, a);
+    if (a.D <= 512) hipLaunchKernelGGL((rms_norm_bwd<64, 1, FP32>), dim3(groups), dim3(norm_back_threads(64)), 0, s, a);
+    else if (a.D <= 1024) hipLaunchKernelGGL((rms_norm_bwd<64, 2, FP32>), dim3(groups), dim3(norm_back_threads(64)), 0, s, a);
+    else if (a.D <= 2048) hipLaunchKernelGGL((rms_norm_bwd<64, 4, FP32>), dim3(groups), dim3(norm_back_threads(64)), 0, s, a);
     else if (a.D <= 4096) hipLaunchKernelGGL((rms_norm_bwd<256, 2, FP32>), dim3(groups), dim3(256), 0, s, a);
     else if (a.D <= 8192) hipLaunchKernelGGL((rms_norm_bwd<256, 4, FP32>), dim3(groups), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((rms_norm_bwd<1024, 2, FP32>), dim3(groups), dim3(1024), 0, s, a);
@@ -372,7 +380,7 @@ int ws_rms_norm_bwd(const float* dY, int64_t lddy, const void* h, int64_t ldh, c
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (stream_bytes == 4) launch_norm_back<true>(a, groups, s);
     else launch_norm_back<false>(a, groups, s);
-    if (dgamma) hipLaunchKernelGGL(rms_norm_dgamma, dim3(D / 32), dim3(1024), 0, s, a.parts, groups, D, dgamma);
+    if (dgamma) hipLaunchKernelGGL(rms_norm_dgamma, dim3(D / 32), dim3(256), 0, s, a.parts, groups, D, dgamma);
     return hipGetLastError() == hipSuccess ? WS_OK : WS_ERR_HIP;
 }
 
