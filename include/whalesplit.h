@@ -311,8 +311,11 @@ int ws_rms_norm_bwd(const float* dY, int64_t lddy, const void* h, int64_t ldh, c
  *                          for ws_split_fc_top1 and ws_combine_top1; workspace of ws_w4_top1_workspace_bytes
  * X_scales NULL: X is bf16 [B][ldx], ldx in elements.  Else X is e4m3 [B][ldx] with scales [B][ldxs].  Weights and features are
  * multiplied as the values they stand for, with fp32 sums; a product of value and scale beyond bf16's range is not supported.
- * No matrix is limited to 4 GiB here; at most WS_W4_MAX_ROWS rows to a call (else WS_ERR_SHAPE). */
+ * No matrix is limited to 4 GiB here; at most WS_W4_MAX_ROWS rows to a call and WS_W4_MAX_PITCH bytes to a pitch of codes or
+ * scales (else WS_ERR_SHAPE), and at most WS_W4_MAX_CLASSES classes to a shard (else WS_ERR_RANGE). */
 #define WS_W4_MAX_ROWS (1 << 20)
+#define WS_W4_MAX_PITCH (1 << 26)
+#define WS_W4_MAX_CLASSES ((1 << 30) - 65536)
 int ws_quantize_mx4(const void* W, int64_t ldw, int32_t C, int32_t D, void* W4, int64_t ldw4,
                     void* W_scales, int64_t lds, void* stream);
 int ws_split_fc_w4_logits(const void* X, int64_t ldx, const void* X_scales, int64_t ldxs,

@@ -56,23 +56,10 @@ struct W4Args {
     float* part_val; int* part_cls;          // [B][workgroups along the classes]
 };
 
-constexpr int W4_MAX_ROWS = WS_W4_MAX_ROWS;  // row tiles are counted in the grid's second extent
-constexpr int64_t W4_MAX_PITCH = 1 << 26;      // 16 rows are addressed with 31 bits
+constexpr int W4_MAX_ROWS = WS_W4_MAX_ROWS;
+constexpr int64_t W4_MAX_PITCH = WS_W4_MAX_PITCH;                            // 16 rows are addressed with 31 bits
+constexpr int W4_MAX_CLASSES = WS_W4_MAX_CLASSES;                            // a whole last group's biases are addressed with 32 bits
 constexpr int W4_STEP = 128;                 // features that the lanes of a wave cover with 16 bytes of codes each
-
-// How a call is cut: a wave takes CT x 16 classes and NT x 16 rows, a workgroup WAVES waves along the classes; the codes of PIECE steps
-// are loaded while those of the PIECE before are multiplied.
-template <int NT_> struct W4Shape {
-    static constexpr int NT = NT_;
-    static constexpr int CT = NT <= 2 ? 1 : 2;
-    static constexpr int WAVES = NT <= 2 ? 4 : 8;
-    static constexpr int PIECE = NT <= 2 ? 4 : NT <= 4 ? 2 : 1;
-    static constexpr int ROWS = 16 * NT, THREADS = 64 * WAVES, CLASSES = 16 * CT * WAVES;
-};
-
-// Steps of `rows` rows of features that 80 KiB hold, so that two workgroups share a compute unit.
-constexpr int W4_LDS = 81920;
-constexpr int w4_chunk(int rows) { return ((W4_LDS / 4 - 256) / rows - 16) / 64; }
 
 // Where a lane loads and where its data goes.  A load takes 16 bytes of codes a lane, four neighbouring lanes 64 bytes of a class row: 16 rows x 64
 // bytes, one step of 16 classes.  With a lane for each row, as the matrix instruction has them, every lane is in a cache line of its own and
@@ -107,7 +94,7 @@ struct W4Tile {
 template <int N> struct W4Piece {
     static constexpr int HELD = (N + 3) / 4;
     u32x4 v[N];
-    uint32_t s[HELD], t[HELD];               // two scales each
+    uint16_t s[HELD], t[HELD];               // two scales each
 };
 
 // From feature k on (a step's first).  Beyond the row's end it may read the next row's bytes: codes stand for numbers whatever they are, and the
@@ -128,7 +115,8 @@ __device__ __forceinline__ void w4_load(W4Piece<N>& p, const W4Tile& tile, const
 template <int N>
 __device__ __forceinline__ void w4_join(uint32_t (&joined)[W4Piece<N>::HELD], const W4Piece<N>& p) {
 #pragma unroll
-    for (int j = 0; j < W4Piece<N>::HELD; ++j) asm volatile("v_lshl_or_b32 %0, %1, 16, %2" : "=v"(joined[j]) : "v"(p.t[j]), "v"(p.s[j]));
+    for (int j = 0; j < W4Piece<N>::HELD; ++j)
+        asm volatile("v_perm_b32 %0, %1, %2, %3" : "=v"(joined[j]) : "v"(p.t[j]), "v"(p.s[j]), "s"(0x05040100));
 }
 
 // The lane's codes and scale of step i for the product, of which `left` features from step 0 on are there (a multiple of 64).
@@ -227,20 +215,29 @@ __device__ __forceinline__ void w4_multiply(f32x4 (&acc)[CT][NT], const W4Piece<
     else w4_multiply_steps<false>(acc, p, x, at, left, l);
 }
 
-// Four classes' biases; zeros without a bias and beyond the shard.
-__device__ __forceinline__ f32x4 w4_bias(const W4Args& a, int cls) {
-    f32x4 b = {0.f, 0.f, 0.f, 0.f};
-    if (a.bias != nullptr)
+// The biases as a buffer, zeros without a bias and beyond the shard; four classes' from class cls on.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t w4_biases(const W4Args& a) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.bias), 0, a.bias != nullptr ? (int)(4u * (uint32_t)a.C) : 0, 0x00020000);
+}
+__device__ __forceinline__ f32x4 w4_bias(__amdgpu_buffer_rsrc_t biases, int cls) {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, 4 * cls, 0, 0));
+}
+
+// Four neighbouring logits, of which the first `n` (any number) are there.
+__device__ __forceinline__ void w4_store(float* z, f32x4 v, int n) {
+    if (n >= 4) {
+        *reinterpret_cast<f32x4*>(z) = v;
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (cls + e < a.C) b[e] = a.bias[cls + e];
-    return b;
+        for (int e = 0; e < 3; ++e)
+            if (e < n) z[e] = v[e];
+    }
 }
 
 // The logits of four neighbouring classes of 16 NT rows: stored, or held against the best so far.
 template <int NT, bool TOP1>
-__device__ __forceinline__ void w4_finish(const W4Args& a, const f32x4 (&acc)[NT], f32x4 b, int cls, int row0, int rows, int i16, float (&best)[NT],
-                                          int (&best_at)[NT]) {
+__device__ __forceinline__ void w4_finish(const W4Args& a, const f32x4 (&acc)[NT], f32x4 b, int cls, int row0, int rows, int i16, float* best,
+                                          int* best_at) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const f32x4 v = acc[n] + b;
@@ -251,21 +248,14 @@ __device__ __forceinline__ void w4_finish(const W4Args& a, const f32x4 (&acc)[NT
         } else {
             const int r = 16 * n + i16;
             if (r >= rows) continue;
-            float* z = a.Z + (int64_t)(row0 + r) * a.ldz + cls;
-            if (cls + 4 <= a.C) {
-                *reinterpret_cast<f32x4*>(z) = v;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (cls + e < a.C) z[e] = v[e];
-            }
+            w4_store(a.Z + (int64_t)(row0 + r) * a.ldz + cls, v, a.C - cls);
         }
     }
 }
 
 // The workgroup's candidates of its rows, out of its lanes' and waves'.
 template <int NT, int WAVES>
-__device__ __forceinline__ void w4_report(const W4Args& a, float (&best)[NT], int (&best_at)[NT], int row0, int rows, const W4Lane& l, char* lds) {
+__device__ __forceinline__ void w4_report(const W4Args& a, float (&best)[NT], int (&best_at)[NT], int row0, int rows, const W4Lane& l, char* lds, int part, int parts) {
     constexpr int R = 16 * NT;
     __syncthreads();                                                           // the features have been read
     float* sv = reinterpret_cast<float*>(lds);
@@ -286,71 +276,221 @@ __device__ __forceinline__ void w4_report(const W4Args& a, float (&best)[NT], in
         int at = sc[tid];
 #pragma unroll
         for (int k = 1; k < WAVES; ++k) better_of(v, at, sv[k * R + tid], sc[k * R + tid]);
-        a.part_val[(int64_t)(row0 + tid) * gridDim.x + blockIdx.x] = v;
-        a.part_cls[(int64_t)(row0 + tid) * gridDim.x + blockIdx.x] = at;
+        a.part_val[(int64_t)(row0 + tid) * parts + part] = v;
+        a.part_cls[(int64_t)(row0 + tid) * parts + part] = at;
     }
 }
 
-// `chunk` steps of the features are in LDS at a time.
-template <int NT, bool MX, bool TOP1>
-__global__ __launch_bounds__(W4Shape<NT>::THREADS) void w4_product(W4Args a, int chunk, int groups) {
-    typedef W4Shape<NT> S;
-    constexpr int CT = S::CT, PIECE = S::PIECE, R = S::ROWS, WAVES = S::WAVES;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+// ---- many rows ---------------------------------------------------------------------------------------------------------
+// A wave takes CT x 16 classes and 16 NT rows, a workgroup WAVES waves along the classes; tile c of all waves makes WAVES x 16 neighbouring classes.
+// A step of the rows' features is in LDS, the next one on its way to the other half, and so are the next codes.  A step takes 2.2 us with 64
+// rows, most of it the way of its codes: load, exchange between lanes, conversion, product; with 256 rows the matrix instructions and LDS, from which
+// every wave reads every feature fragment, for CT products each.  200 x 1088 x 50 001: 39.8 us, 128 x 2048 x 100 000: 65 (800 TFLOP/s), 256: 122 (860).
+// Up to 64 rows CT = 2 leaves registers for two workgroups on a compute unit, which fill each other's pauses (64 x 256 x 100 000 classes 15.2 us,
+// CT = 4 17.8); with more rows CT = 4 halves what is read from LDS for a product.
+//
+// Tried and slower: the codes of two steps on their way (64 x 2048 x 100 000 classes 48.8 us, now 47.4); the scales of 16 steps through LDS
+// (a step of 64 rows is 15 % faster, but the start costs 7 us: 200 x 1088 x 50 001 49.6 us, now 39.8).
+//
+// Logits leave through LDS, one c after the other, in a loop that is not unrolled: straight from the accumulators every one of the CT NT 4 stores
+// and bounds checks is code of its own, 10 KiB that each launch fetches anew (128 rows x 256 features x 100 000 classes 28.6 us).
+template <int NT, int CT, int WAVES, bool MX, bool TOP1>
+__global__ __launch_bounds__(64 * WAVES, CT == 2 && WAVES == 8 ? 4 : 2) void w4_tiles(W4Args a, int groups, int row_blocks, int parts) {
+    constexpr int R = 16 * NT, THREADS = 64 * WAVES, STRIP = 16 * WAVES, CLASSES = CT * STRIP;
+    constexpr int PITCH = 64 + 16, PLANE = (R * PITCH + 255) & ~255, HALF = 4 * PLANE;
+    constexpr int OUT_PITCH = STRIP + 4;                                           // floats
+    constexpr int OUT_BYTES = R * OUT_PITCH * 4;
+    constexpr int UNITS = (R * 8 + THREADS - 1) / THREADS;                         // of 16 features that a thread brings to LDS in a step
+    constexpr bool EARLY = CT * NT <= 24;                                          // registers for the next step's codes in the product's order, too
+    __shared__ __attribute__((aligned(16))) char lds[2 * HALF > OUT_BYTES ? 2 * HALF : OUT_BYTES];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const W4Lane l(tid & 63, a);
-    const int i16 = l.i16, g = l.g;
-    const int row0 = blockIdx.y * R;
+    // the row blocks of a group of classes run on one XCD one after the other, and find its codes in that L2
+    const int slot = blockIdx.x >> 3, block = slot % row_blocks, first = (blockIdx.x & 7) + 8 * (slot / row_blocks);
+    if (first >= parts) return;
+    const int row0 = block * R;
     const int rows = a.B - row0 < R ? a.B - row0 : R;
-    const int pitch = 64 * chunk + 16, plane = (rows * pitch + 255) & ~255;
-    // rows beyond the batch and classes beyond the shard repeat the last one: nothing of them is kept
-    const char* x[NT];
+    const int steps = (a.D + W4_STEP - 1) / W4_STEP;
+    const char* x = lds + l.g * PLANE + l.i16 * PITCH;                             // rows beyond the batch stay as LDS has them: nothing of them is kept
+    const __amdgpu_buffer_rsrc_t biases = w4_biases(a);
+    // in the output loop QUADS threads share a row, and a thread takes four classes of every PER-th row
+    constexpr int QUADS = STRIP / 4, PER = THREADS / QUADS, TURNS = R / PER;
+    static_assert(QUADS <= 64 && R % PER == 0, "");
+    const int out_row = tid / QUADS, out_quad = tid % QUADS;
+    float best[TOP1 ? TURNS : 1];
+    int best_at[TOP1 ? TURNS : 1];
+    if constexpr (TOP1)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) x[n] = lds + g * plane + (16 * n + i16 < rows ? 16 * n + i16 : rows - 1) * pitch;
-    float best[NT];
-    int best_at[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        best[n] = -INFINITY;
-        best_at[n] = INT_MAX;
-    }
-    const bool whole = chunk * W4_STEP >= a.D;                                 // staged once for all groups
+        for (int j = 0; j < TURNS; ++j) {
+            best[j] = -INFINITY;
+            best_at[j] = INT_MAX;
+        }
 
-    for (int group = blockIdx.x; group < groups; group += gridDim.x) {
-        const int class0 = group * S::CLASSES + wave * 16 * CT;
+    // this thread's units of a step
+    const uint8_t* from[UNITS];
+    const uint8_t* from_scale[UNITS];
+    int to[UNITS];
+#pragma unroll
+    for (int j = 0; j < UNITS; ++j) {
+        const int u = tid + THREADS * j, r = u >> 3, c = u & 7;
+        const int64_t row = row0 + (r < rows ? r : rows - 1);
+        from[j] = a.X + row * a.ldx + (MX ? 16 : 32) * c;
+        from_scale[j] = MX ? a.xs + row * a.ldxs + (c >> 1) : nullptr;
+        to[j] = r < rows ? ((c >> 1) & 3) * PLANE + r * PITCH + (c & 1) * 32 : -1;
+    }
+    struct Rows {
+        u32x4 a[UNITS], b[UNITS];
+        uint32_t s[UNITS];
+    } coming;
+    // No branch around the loads; beyond the row's end, half a step at most, the last features are loaded once more and zeros are staged.
+    auto fetch = [&](Rows& w, int step) {
+        const int s = step < steps ? step : steps - 1;
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) {
+            const int c = (tid + THREADS * j) & 7;
+            const int back = s * W4_STEP + 16 * c < a.D ? 0 : 64;
+            const u32x4* p = reinterpret_cast<const u32x4*>(from[j] + (MX ? 1 : 2) * (s * W4_STEP - back));
+            w.a[j] = p[0];
+            if constexpr (MX) w.s[j] = from_scale[j][s * 4 - back / 32];
+            else w.b[j] = p[1];
+        }
+    };
+    auto stage = [&](const Rows& w, int step) {
+#pragma unroll
+        for (int j = 0; j < UNITS; ++j) {
+            if (to[j] < 0) continue;
+            const int c = (tid + THREADS * j) & 7;
+            u32x4 lo = w.a[j], hi = w.b[j];
+            if constexpr (MX) {
+                const float f = scale_of(w.s[j], 0);
+                lo = w4_features(w.a[j][0], w.a[j][1], f);
+                hi = w4_features(w.a[j][2], w.a[j][3], f);
+            }
+            if (step * W4_STEP + 16 * c >= a.D) lo = hi = u32x4{0, 0, 0, 0};
+            u32x4* q = reinterpret_cast<u32x4*>(lds + (step & 1) * HALF + to[j]);
+            q[0] = lo;
+            q[1] = hi;
+        }
+    };
+
+    for (int group = first; group < groups; group += parts) {
+        const int class0 = group * CLASSES + wave * 16;
+        W4Piece<1> codes[CT];
+        auto load = [&](int step) {
+#pragma unroll
+            for (int c = 0; c < CT; ++c) w4_load(codes[c], W4Tile(a, class0 + STRIP * c), l, step * W4_STEP);
+        };
+        float f[CT];                                                               // codes and scales in the product's order
+        u32x4 v[CT];
+        auto take = [&](float (&to_f)[CT], u32x4 (&to_v)[CT], int c, int step) {
+            uint32_t joined[1];
+            w4_join(joined, codes[c]);
+            to_f[c] = w4_scale<false>(joined, 0, a.D - step * W4_STEP, l);
+            to_v[c] = w4_codes(codes[c], 0, l);
+        };
         f32x4 acc[CT][NT];
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int n = 0; n < NT; ++n) acc[c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-        W4Piece<PIECE> even[CT], odd[CT];
-        auto load = [&](W4Piece<PIECE> (&p)[CT], int k) {
+        fetch(coming, 0);
+        load(0);
+        stage(coming, 0);
+        if constexpr (EARLY) {
 #pragma unroll
-            for (int c = 0; c < CT; ++c) w4_load(p[c], W4Tile(a, class0 + 16 * c), l, k);
-        };
-        load(even, 0);
-        for (int k0 = 0; k0 < a.D; k0 += chunk * W4_STEP) {
-            if (!whole || group == (int)blockIdx.x) {
-                if (k0 > 0 || group != (int)blockIdx.x) __syncthreads();       // the chunk before has been read
-                const int left = (a.D - k0 + W4_STEP - 1) / W4_STEP;
-                w4_stage<S::THREADS, MX>(a, row0, rows, k0, left < chunk ? left : chunk, lds, pitch, plane);
-                __syncthreads();
+            for (int c = 0; c < CT; ++c) take(f, v, c, 0);
+            load(1);
+        }
+        wait_counts<NO_VM_WAIT, 0>();
+        raw_barrier();
+#pragma unroll 1
+        for (int step = 0; step < steps; ++step) {
+            fetch(coming, step + 1);
+            if constexpr (!EARLY) {
+#pragma unroll
+                for (int c = 0; c < CT; ++c) take(f, v, c, step);
+                load(step + 1);
             }
-            const int end = k0 + chunk * W4_STEP < a.D ? k0 + chunk * W4_STEP : a.D;
-            for (int k = k0; k < end; k += 2 * PIECE * W4_STEP) {
-                constexpr int SPAN = PIECE * W4_STEP;
-                load(odd, k + SPAN);
-                w4_multiply_steps<false>(acc, even, x, (k - k0) / 2, a.D - k, l);
-                load(even, k + 2 * SPAN);
-                if (k + SPAN < end) w4_multiply_steps<false>(acc, odd, x, (k - k0) / 2 + 64 * PIECE, a.D - k - SPAN, l);
+            // Fragments of the features are read three ahead, and the codes of the next quarter of a step turned into values meanwhile; the order is
+            // pinned, left alone the reads end up right in front of their products and the loads behind them.
+            const char* at = x + (step & 1) * HALF;
+            auto fragment = [&](int i) { return *reinterpret_cast<const bf16x8*>(at + 16 * PITCH * (i % NT) + 16 * (i / NT)); };
+            bf16x8 ring[4], wa[CT], ahead[CT];
+            float next_f[CT];
+            u32x4 next_v[CT];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) ring[i] = fragment(i);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) wa[c] = w4_values(v[c][0], f[c]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 4 * NT; ++i) {
+                const int q = i / NT, n = i % NT;
+                if (i + 3 < 4 * NT) ring[(i + 3) & 3] = fragment(i + 3);
+                if (q < 3)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+                        if (c % NT == n) ahead[c] = w4_values(v[c][q + 1], f[c]);
+                if (EARLY && q >= 2)                                               // the next step's codes, a tile at a time in the second half of this one
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+                        if (c == (i - 2 * NT) * CT / (2 * NT) && (i == 2 * NT || c != (i - 1 - 2 * NT) * CT / (2 * NT))) take(next_f, next_v, c, step + 1);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) acc[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[c], ring[i & 3], acc[c][n], 0, 0, 0);
+                if (n == NT - 1)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) wa[c] = ahead[c];
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (EARLY) {
+                load(step + 2);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    f[c] = next_f[c];
+                    v[c] = next_v[c];
+                }
+            }
+            stage(coming, step + 1);
+            wait_counts<NO_VM_WAIT, 0>();
+            raw_barrier();                                                         // the codes stay in flight
+        }
+        float* out = reinterpret_cast<float*>(lds);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) *reinterpret_cast<f32x4*>(out + (16 * n + l.i16) * OUT_PITCH + 16 * wave + 4 * l.g) = acc[c][n];
+            const int cls = group * CLASSES + STRIP * c + 4 * out_quad;
+            const f32x4 bias = w4_bias(biases, cls);
+            __syncthreads();
+            if constexpr (TOP1) {
+#pragma unroll
+                for (int j = 0; j < TURNS; ++j) {
+                    const f32x4 z = *reinterpret_cast<const f32x4*>(out + (out_row + j * PER) * OUT_PITCH + 4 * out_quad) + bias;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (cls + e < a.C) better_of(best[j], best_at[j], z[e], cls + e);
+                }
+            } else {
+#pragma unroll 1
+                for (int r = out_row; r < rows; r += PER) {
+                    const f32x4 z = *reinterpret_cast<const f32x4*>(out + r * OUT_PITCH + 4 * out_quad) + bias;
+                    w4_store(a.Z + (int64_t)(row0 + r) * a.ldz + cls, z, a.C - cls);
+                }
+            }
+            __syncthreads();
+        }
+    }
+    if constexpr (TOP1) {
+#pragma unroll
+        for (int j = 0; j < TURNS; ++j) {
+            for (int m = 1; m < QUADS; m <<= 1) better_of(best[j], best_at[j], __shfl_xor(best[j], m, 64), __shfl_xor(best_at[j], m, 64));
+            const int r = out_row + j * PER;
+            if (out_quad == 0 && r < rows) {
+                a.part_val[(int64_t)(row0 + r) * parts + first] = best[j];
+                a.part_cls[(int64_t)(row0 + r) * parts + first] = best_at[j];
             }
         }
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-            w4_finish<NT, TOP1>(a, acc[c], w4_bias(a, class0 + 16 * c + 4 * g), class0 + 16 * c + 4 * g, row0, rows, i16, best, best_at);
     }
-    if constexpr (TOP1) w4_report<NT, WAVES>(a, best, best_at, row0, rows, l, lds);
 }
 
 // ---- few rows, many classes --------------------------------------------------------------------------------------------
@@ -378,8 +518,7 @@ __global__ __launch_bounds__(W4_STREAM_THREADS) void w4_stream(W4Args a, int til
     W4Piece<PIECE> ring[RING][1];
     f32x4 bias[RING];                                                              // of the tile that ends with this piece
     W4Tile aim(a, 16 * tile);
-    const __amdgpu_buffer_rsrc_t biases =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.bias), 0, a.bias != nullptr ? (int)(4u * (uint32_t)a.C) : 0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t biases = w4_biases(a);
     auto load = [&](int i) {
         w4_load(ring[i][0], aim, l, k);
         k += SPAN;
@@ -426,7 +565,7 @@ __global__ __launch_bounds__(W4_STREAM_THREADS) void w4_stream(W4Args a, int til
             load(i);
         }
     }
-    if constexpr (TOP1) w4_report<NT, W4_STREAM_WAVES>(a, best, best_at, 0, rows, l, lds);
+    if constexpr (TOP1) w4_report<NT, W4_STREAM_WAVES>(a, best, best_at, 0, rows, l, lds, blockIdx.x, gridDim.x);
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------------------
@@ -434,8 +573,8 @@ __global__ __launch_bounds__(W4_STREAM_THREADS) void w4_stream(W4Args a, int til
 // meet in LDS.  One workgroup per group of classes, most of a compute unit's wave slots filled with them: reading alone, W of 100 000 x 2048
 // takes 16.9 us so, 19.9 with a wave for 16 whole rows; 1000 x 4096 2.8 and 6.8.
 //
-// WK = 1 << wk_shift waves along the contraction, wave k the steps S k .. S k + S - 1; the 8 / WK groups of waves take CT tiles of 16 classes
-// each.  Rows go 16 at a time, and P steps of them at a time through LDS, where each wave has a region of its own.
+// Wave k takes the steps S k .. S k + S - 1 of CT tiles of 16 classes.  Rows go 16 at a time, and P steps of them at a time through LDS, where
+// each wave has a region of its own.
 constexpr int W4_FEW_ROWS = 64;
 constexpr int W4_FEW_WAVES = 8, W4_FEW_THREADS = 64 * W4_FEW_WAVES;
 constexpr int w4_few_piece(int S, int CT, bool MX) { return S >= 2 && S <= 4 && (MX || CT * S == 2) ? 2 : 1; }          // P, as many as the registers hold
@@ -446,24 +585,24 @@ constexpr int w4_few_region(int P, int CT, int rows) {
 }
 
 template <int S, int CT, bool MX, bool TOP1>
-__global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4Args a, int wk_shift) {
+__global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4Args a) {
     constexpr int P = w4_few_piece(S, CT, MX), PITCH = 16 * CT + 4, UNITS = MX ? P * 2 : P * 4;        // 16-byte loads of a lane for a piece of 16 rows
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63;
     const W4Lane l(lane, a);
     const int i16 = l.i16, g = l.g;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int WK = 1 << wk_shift, part = wave >> wk_shift;
-    const int step0 = (wave & (WK - 1)) * S;
+    const int step0 = wave * S;
     const int most = a.B < 16 ? a.B : 16;
     const int plane = w4_few_plane(P, most), region = w4_few_region(P, CT, most);
     char* mine = lds + wave * region;
-    const int first = (blockIdx.x << (3 - wk_shift)) * 16 * CT;                    // the workgroup's first class
-    // this thread's four neighbouring classes in the sum over the waves, of every (512 / quads)-th row
-    const int quads = (4 * CT) << (3 - wk_shift), c4 = tid & (quads - 1);
+    const int first = blockIdx.x * 16 * CT;                                        // the workgroup's first class
+    // this thread's four neighbouring classes in the sum over the waves, of every (512 / QUADS)-th row
+    constexpr int QUADS = 4 * CT;
+    const int c4 = tid & (QUADS - 1);
     const int cls = first + 4 * c4;
 
-    const f32x4 bias = w4_bias(a, cls);
+    const f32x4 bias = w4_bias(w4_biases(a), cls);
 
     // features [8 u, 8 u + 8) (MX: 16) of a piece and row, as the lane's load j: u + units per row * row = lane + 64 j
     constexpr int ROW_UNITS = MX ? 8 * P : 16 * P;
@@ -504,7 +643,7 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4A
     if (busy) fetch(0, 0);                                                         // from the cache, and staged while the codes are on their way
     W4Piece<S> codes[CT];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) w4_load(codes[c], W4Tile(a, busy ? first + 16 * (part * CT + c) : a.C), l, step0 * W4_STEP);
+    for (int c = 0; c < CT; ++c) w4_load(codes[c], W4Tile(a, busy ? first + 16 * c : a.C), l, step0 * W4_STEP);
     for (int n0 = 0; n0 < a.B; n0 += 16) {
         const int rows = a.B - n0 < 16 ? a.B - n0 : 16;
         f32x4 acc[CT];
@@ -552,10 +691,10 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4A
         }
         wait_counts<NO_VM_WAIT, 0>();
         raw_barrier();                                                             // loads stay in flight
-        const char* from = lds + ((c4 / (4 * CT)) << wk_shift) * region + 16 * (c4 & (4 * CT - 1));
-        for (int r = tid / quads; r < rows; r += W4_FEW_THREADS / quads) {
+        const char* from = lds + 16 * c4;
+        for (int r = tid / QUADS; r < rows; r += W4_FEW_THREADS / QUADS) {
             f32x4 z = *reinterpret_cast<const f32x4*>(from + r * PITCH * 4);
-            for (int k = 1; k < WK; ++k) z += *reinterpret_cast<const f32x4*>(from + k * region + r * PITCH * 4);
+            for (int k = 1; k < W4_FEW_WAVES; ++k) z += *reinterpret_cast<const f32x4*>(from + k * region + r * PITCH * 4);
             z += bias;
             if constexpr (TOP1) {
                 float best = -INFINITY;
@@ -563,20 +702,13 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4A
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (cls + e < a.C) better_of(best, at, z[e], cls + e);
-                for (int m = 1; m < quads; m <<= 1) better_of(best, at, __shfl_xor(best, m, 64), __shfl_xor(at, m, 64));       // a row's lanes are neighbours
+                for (int m = 1; m < QUADS; m <<= 1) better_of(best, at, __shfl_xor(best, m, 64), __shfl_xor(at, m, 64));       // a row's lanes are neighbours
                 if (c4 == 0) {
                     a.part_val[(int64_t)(n0 + r) * gridDim.x + blockIdx.x] = best;
                     a.part_cls[(int64_t)(n0 + r) * gridDim.x + blockIdx.x] = at;
                 }
             } else {
-                float* out = a.Z + (int64_t)(n0 + r) * a.ldz + cls;
-                if (cls + 4 <= a.C) {
-                    *reinterpret_cast<f32x4*>(out) = z;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (cls + e < a.C) out[e] = z[e];
-                }
+                w4_store(a.Z + (int64_t)(n0 + r) * a.ldz + cls, z, a.C - cls);
             }
         }
         if (n0 + 16 < a.B) {
@@ -611,82 +743,89 @@ __global__ __launch_bounds__(256) void w4_merge_top1(const float* __restrict__ v
 
 static inline bool al(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-// Rows are cut evenly into blocks of at most eight tiles of 16.
-static int w4_row_tiles(int B) {
-    const int tiles = (B + 15) / 16, blocks = (tiles + 7) / 8;
-    return (tiles + blocks - 1) / blocks;
-}
-
 // How a call is run.  us of the launch, fp32 logits of bf16 features, codes not in any cache (one MI355X):
-//   rows x features x classes    w4_stream RING 1, 2    w4_few       w4_product
-//    1 x 2048 x 100000           24.0  24.9             29           26
-//   16 x 2048 x 100000           27.0  27.2             31           39
-//   32 x 2048 x 100000           31.4  33.9             47           57
-//    1 x  512 x 100000            8.2  10.3             10.7          9.5
-//    1 x 2048 x 12500             8.2   7.6              7.0          7.6
-//   32 x 2048 x 12500            12.2  11.3             11.2         15.9
-//   64 x 2048 x 12500                                   16.9         30.9
-//   64 x 2048 x 100000                                  75           62
-//    1 x 8192 x 12500            24.5  17.0             28           19.6
+//   rows x features x classes    w4_stream RING 1, 2    w4_few       w4_tiles
+//    1 x 2048 x 100000           24.0  24.9             29           35
+//   16 x 2048 x 100000           27.0  27.2             31           37
+//   32 x 2048 x 100000           31.4  33.9             47           40
+//    1 x  512 x 100000            8.2  10.3             10.7         11.9
+//    1 x 2048 x 12500             8.2   7.6              7.0         14.0
+//   32 x 2048 x 12500            12.2  11.3             11.2         15.1
+//    1 x 8192 x 12500            24.5  17.0             28           47
 //    1 x 4096 x 4000             10.3   8.9              5.4
-//    1 x 4096 x 1000             10.1   8.6              4.8          8.9
+//    1 x 4096 x 1000             10.1   8.6              4.8         19.1
 //    8 x  512 x 2000              3.2   4.8              3.9
+//   40 x 2048 x 12500                                   14.0         17.1
+//   64 x  512 x 12500                                   10.0          7.8
+//   64 x 2048 x 3000                                    10.1         16.1
+//   64 x 2048 x 12500                                   18.5         18.9
+//   64 x 2048 x 25000                                   25.3         20.5
+//   64 x 2048 x 100000                                  75           47.6
 // A wave of w4_stream takes whole rows of 16 classes: with few of them most waves have nothing to do, and w4_few shares the rows out.  Its second
-// barrier-bound half costs some 3 us, so short rows and many classes stay on w4_stream.
-enum W4Way { W4_STREAM, W4_FEW, W4_PRODUCT };
+// barrier-bound half costs some 3 us, so short rows and many classes stay on w4_stream, or with more rows than it holds on w4_tiles.
+enum W4Way { W4_STREAM, W4_FEW, W4_TILES };
 struct W4Plan {
     W4Way way;
     int groups;                              // workgroups along the classes
     int ring;                                // w4_stream
-    int S, CT, wk_shift;                     // w4_few
+    int S, CT;                               // w4_few
+    int NT;                                  // w4_tiles
+    bool wide;                               //   eight waves, not four
 };
+constexpr int W4_MAX_PARTS = 4096;           // candidates of a row at most
 constexpr size_t W4_STREAM_LDS = 160 * 1024;
 static size_t w4_stream_lds(int B, int D) {
     const size_t steps = (D + W4_STEP - 1) / W4_STEP;
     return 4 * (((size_t)B * (64 * steps + 16) + 255) & ~(size_t)255);
 }
-static W4Plan w4_plan(int B, int D, int C) {
-    W4Plan p = {W4_PRODUCT, 0, 1, 1, 1, 3};
+static W4Plan w4_plan(int B, int D, int C, bool top1) {
+    W4Plan p = {W4_TILES, 0, 1, 1, 1, 0, false};
     const int64_t tiles = ((int64_t)C + 15) / 16;
     const int steps = (D + W4_STEP - 1) / W4_STEP;
     const bool fits = B <= 32 && w4_stream_lds(B, D) <= W4_STREAM_LDS;
     const int64_t most = steps <= 32 ? 1024 : 512;                                 // tiles up to which rows are shared out
-    if (B <= W4_FEW_ROWS && steps <= 8 * W4_FEW_WAVES && (fits ? steps >= 8 && tiles <= most : tiles * ((B + 15) / 16) <= 4 * most)) {
+    if (B <= W4_FEW_ROWS && steps >= 8 && steps <= 8 * W4_FEW_WAVES && (fits ? tiles <= most : tiles * ((B + 15) / 16) <= 4 * most)) {
         p.way = W4_FEW;
         while (W4_FEW_WAVES * p.S < steps) p.S *= 2;
-        while (p.wk_shift > 0 && (1 << (p.wk_shift - 1)) * p.S >= steps) --p.wk_shift;
         // as many classes to a workgroup as the registers hold, while there are workgroups for most compute units
-        p.CT = p.S == 1 ? (p.wk_shift == 0 ? 2 : 4) : p.S == 2 ? 4 : p.S == 4 ? 2 : 1;
+        p.CT = p.S <= 2 ? 4 : p.S == 4 ? 2 : 1;
         if (p.S > 1 && tiles < 192 * p.CT) p.CT = 1;
-        const int64_t at_once = (int64_t)p.CT << (3 - p.wk_shift);
-        p.groups = (int)((tiles + at_once - 1) / at_once);
+        p.groups = (int)((tiles + p.CT - 1) / p.CT);
     } else if (fits) {
         p.way = W4_STREAM;
         p.groups = tiles < 256 ? (int)tiles : 256;
         p.ring = steps > 32 && tiles <= 1024 ? 2 : 1;
+    } else {
+        const int row_tiles = (B + 15) / 16;
+        auto padded = [&](int nt) { return (row_tiles + nt - 1) / nt * nt; };
+        p.NT = row_tiles <= 2 ? 2 : row_tiles <= 4 || top1 ? 4 : padded(6) < padded(8) ? 6 : 8;      // the rows' candidates take registers, too
+        const int wide = p.NT <= 4 ? 16 : 32;
+        p.wide = (tiles + wide - 1) / wide * (padded(p.NT) / p.NT) >= 160;
+        if (!p.wide && p.NT > 4) p.NT = 4;
+        const int at_once = p.wide ? wide : 8;
+        p.groups = (int)((tiles + at_once - 1) / at_once);
     }
     return p;
 }
 
-static int w4_classes(int B) { return w4_row_tiles(B) <= 2 ? W4Shape<1>::CLASSES : W4Shape<8>::CLASSES; }
-static int w4_groups(int B, int C) { return (int)(((int64_t)C + w4_classes(B) - 1) / w4_classes(B)); }        // of classes that a workgroup takes at a time
-// Workgroups along the classes of the arg-max on w4_product, each with a candidate for every row; they walk the groups.
-constexpr int W4_MAX_PARTS = 4096;
-static int w4_parts(int B, int D, int C) {
-    const W4Plan p = w4_plan(B, D, C);
-    return p.way != W4_PRODUCT ? p.groups : w4_groups(B, C) < W4_MAX_PARTS ? w4_groups(B, C) : W4_MAX_PARTS;
+// Candidates of a row: one of each workgroup along the classes.  w4_tiles' workgroups walk the groups, and with very many rows there are fewer
+// of them: a launch counts its threads with 32 bits.
+static int w4_parts(const W4Plan& p, int B) {
+    int parts = p.groups < W4_MAX_PARTS ? p.groups : W4_MAX_PARTS;
+    if (p.way == W4_TILES)
+        while ((int64_t)parts * ((B + 31) / 32) > 1 << 20) parts /= 2;
+    return parts;
 }
 
 template <int S, int CT, bool MX, bool TOP1>
 static void launch_w4_few(const W4Args& a, const W4Plan& f, hipStream_t s) {
     const size_t bytes = (size_t)W4_FEW_WAVES * w4_few_region(w4_few_piece(S, CT, MX), CT, a.B < 16 ? a.B : 16);
-    hipLaunchKernelGGL((w4_few<S, CT, MX, TOP1>), dim3(f.groups), dim3(W4_FEW_THREADS), bytes, s, a, f.wk_shift);
+    hipLaunchKernelGGL((w4_few<S, CT, MX, TOP1>), dim3(f.groups), dim3(W4_FEW_THREADS), bytes, s, a);
 }
 
 template <bool MX, bool TOP1>
 static void launch_w4_steps(const W4Args& a, const W4Plan& f, hipStream_t s) {
     switch (f.S * 8 + f.CT) {
-        case 1 * 8 + 2: return launch_w4_few<1, 2, MX, TOP1>(a, f, s);
         case 1 * 8 + 4: return launch_w4_few<1, 4, MX, TOP1>(a, f, s);
         case 2 * 8 + 1: return launch_w4_few<2, 1, MX, TOP1>(a, f, s);
         case 2 * 8 + 4: return launch_w4_few<2, 4, MX, TOP1>(a, f, s);
@@ -696,22 +835,11 @@ static void launch_w4_steps(const W4Args& a, const W4Plan& f, hipStream_t s) {
     }
 }
 
-template <int NT, bool MX, bool TOP1>
-static void launch_w4_tiles(const W4Args& a, hipStream_t s) {
-    typedef W4Shape<NT> S;
-    const int rows = a.B < S::ROWS ? a.B : S::ROWS;
-    const int steps = (a.D + W4_STEP - 1) / W4_STEP;
-    // all of them, or whole pairs of pieces: the kernel takes two in turn and a chunk has to hold one pair at least
-    static_assert(w4_chunk(S::ROWS) >= 2 * S::PIECE, "");
-    int chunk = w4_chunk(rows);
-    chunk = chunk >= steps ? steps : chunk / (2 * S::PIECE) * (2 * S::PIECE);
-    const int plane = (rows * (64 * chunk + 16) + 255) & ~255;
-    size_t bytes = 4 * (size_t)plane;
-    const size_t least = TOP1 ? (size_t)S::WAVES * S::ROWS * 8 : 0;
-    if (bytes < least) bytes = least;
-    const int groups = w4_groups(a.B, a.C);
-    hipLaunchKernelGGL((w4_product<NT, MX, TOP1>), dim3(TOP1 ? w4_parts(a.B, a.D, a.C) : groups, (a.B + S::ROWS - 1) / S::ROWS), dim3(S::THREADS), bytes, s, a,
-                       chunk, groups);
+template <int NT, int CT, int WAVES, bool MX, bool TOP1>
+static void launch_w4_tiles(const W4Args& a, const W4Plan& p, hipStream_t s) {
+    const int row_blocks = (a.B + 16 * NT - 1) / (16 * NT), parts = TOP1 ? w4_parts(p, a.B) : p.groups;
+    const int64_t blocks = ((int64_t)parts + 7) / 8 * 8 * row_blocks;
+    hipLaunchKernelGGL((w4_tiles<NT, CT, WAVES, MX, TOP1>), dim3((unsigned)blocks), dim3(64 * WAVES), 0, s, a, p.groups, row_blocks, parts);
 }
 
 template <int NT, int RING, bool MX, bool TOP1>
@@ -724,21 +852,18 @@ static void launch_w4_stream(const W4Args& a, const W4Plan& p, hipStream_t s) {
 
 template <bool MX, bool TOP1>
 static void launch_w4_type(const W4Args& a, hipStream_t s) {
-    const W4Plan p = w4_plan(a.B, a.D, a.C);
+    const W4Plan p = w4_plan(a.B, a.D, a.C, TOP1);
     if (p.way == W4_FEW) return launch_w4_steps<MX, TOP1>(a, p, s);
     if (p.way == W4_STREAM) {
         if (a.B > 16) return launch_w4_stream<2, 1, MX, TOP1>(a, p, s);
         return p.ring == 1 ? launch_w4_stream<1, 1, MX, TOP1>(a, p, s) : launch_w4_stream<1, 2, MX, TOP1>(a, p, s);
     }
-    switch (w4_row_tiles(a.B)) {
-        case 1: return launch_w4_tiles<1, MX, TOP1>(a, s);
-        case 2: return launch_w4_tiles<2, MX, TOP1>(a, s);
-        case 3: return launch_w4_tiles<3, MX, TOP1>(a, s);
-        case 4: return launch_w4_tiles<4, MX, TOP1>(a, s);
-        case 5: return launch_w4_tiles<5, MX, TOP1>(a, s);
-        case 6: return launch_w4_tiles<6, MX, TOP1>(a, s);
-        case 7: return launch_w4_tiles<7, MX, TOP1>(a, s);
-        default: return launch_w4_tiles<8, MX, TOP1>(a, s);
+    if (!p.wide) return p.NT == 2 ? launch_w4_tiles<2, 2, 4, MX, TOP1>(a, p, s) : launch_w4_tiles<4, 2, 4, MX, TOP1>(a, p, s);
+    switch (p.NT) {
+        case 2: return launch_w4_tiles<2, 2, 8, MX, TOP1>(a, p, s);
+        case 4: return launch_w4_tiles<4, 2, 8, MX, TOP1>(a, p, s);
+        case 6: if constexpr (!TOP1) return launch_w4_tiles<6, 4, 8, MX, false>(a, p, s);
+        default: if constexpr (!TOP1) return launch_w4_tiles<8, 4, 8, MX, false>(a, p, s);
     }
 }
 
@@ -753,7 +878,7 @@ static int check_w4(const void* X, int64_t ldx, const void* X_scales, int64_t ld
     if (!X || !W4 || !W_scales) return WS_ERR_NULL;
     if (B <= 0 || D <= 0 || C_shard <= 0 || D % 64 || B > W4_MAX_ROWS) return WS_ERR_SHAPE;
     if (ldw4 > W4_MAX_PITCH || lds > W4_MAX_PITCH) return WS_ERR_SHAPE;
-    if (C_shard > INT32_MAX - 65536) return WS_ERR_RANGE;                       // class ids of a whole last group are counted in 31 bits
+    if (C_shard > W4_MAX_CLASSES) return WS_ERR_RANGE;
     if (ldx < D || (X_scales && ldxs < D / MX_GROUP) || ldw4 < D / 2 || lds < D / MX_GROUP) return WS_ERR_SHAPE;
     if (!al(X, 16) || ldx % (X_scales ? 16 : 8) || !al(W4, 16) || ldw4 % 16 || !al(W_scales, 2) || lds % 2) return WS_ERR_ALIGN;
     if ((X_scales && (!al(X_scales, 2) || ldxs % 2)) || (b_shard && !al(b_shard, 4))) return WS_ERR_ALIGN;
@@ -803,12 +928,11 @@ int ws_split_fc_w4_logits(const void* X, int64_t ldx, const void* X_scales, int6
     return hipGetLastError() == hipSuccess ? WS_OK : WS_ERR_HIP;
 }
 
-// Whatever the number of features: w4_few has at most a workgroup for 16 classes, and 2048 of them for up to 64 rows; w4_stream has fewer.
+// Whatever the number of features: no kernel has more than a candidate for 16 classes, nor more than W4_MAX_PARTS of them.
 size_t ws_w4_top1_workspace_bytes(int32_t B, int32_t C_shard) {
     if (B <= 0 || C_shard <= 0 || B > W4_MAX_ROWS) return 0;
-    const int64_t tiles = ((int64_t)C_shard + 15) / 16, groups = w4_groups(B, C_shard), many = groups < W4_MAX_PARTS ? groups : W4_MAX_PARTS;
-    const int64_t few = B > W4_FEW_ROWS ? 0 : tiles < W4_MAX_PARTS ? tiles : W4_MAX_PARTS;
-    return (size_t)(few > many ? few : many) * B * 8;
+    const int64_t tiles = ((int64_t)C_shard + 15) / 16;
+    return (size_t)(tiles < W4_MAX_PARTS ? tiles : W4_MAX_PARTS) * B * 8;
 }
 
 int ws_split_fc_w4_top1(const void* X, int64_t ldx, const void* X_scales, int64_t ldxs, const void* W4, int64_t ldw4, const void* W_scales,
@@ -822,7 +946,7 @@ int ws_split_fc_w4_top1(const void* X, int64_t ldx, const void* X_scales, int64_
     if (!workspace || workspace_bytes < ws_w4_top1_workspace_bytes(B, C_shard)) return WS_ERR_WORKSPACE;
     if (!al(workspace, 16)) return WS_ERR_ALIGN;
     W4Args a = w4_args(X, ldx, X_scales, ldxs, W4, ldw4, W_scales, lds, b_shard, B, D, C_shard);
-    const int parts = w4_parts(B, D, C_shard);
+    const int parts = w4_parts(w4_plan(B, D, C_shard, true), B);
     a.part_val = static_cast<float*>(workspace);
     a.part_cls = reinterpret_cast<int*>(a.part_val + (int64_t)parts * B);
     hipStream_t s = static_cast<hipStream_t>(stream);

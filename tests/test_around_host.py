@@ -89,7 +89,8 @@ def test_packing_and_w4_refusals(ws, E):
         assert f(X=A + 8) == E["ALIGN"] and f(ldx=68) == E["ALIGN"] and f(W4=A + 8) == E["ALIGN"] and f(ldw4=36) == E["ALIGN"]
         assert f(xs=A, ldxs=2, ldx=72) == E["ALIGN"] and f(xs=A + 1, ldxs=2) == E["ALIGN"] and f(xs=A, ldxs=3) == E["ALIGN"]
         assert f(s=A + 1) == E["ALIGN"] and f(lds=3) == E["ALIGN"] and f(b=A + 2) == E["ALIGN"]
-        assert f(C=2**31 - 1) == E["RANGE"]
+        assert f(C=2**31 - 1) == E["RANGE"] and f(C=(1 << 30) - 65535) == E["RANGE"]
+        assert f(ldw4=(1 << 26) + 16) == E["SHAPE"] and f(lds=(1 << 26) + 2) == E["SHAPE"]
     assert logits(Z=None) == E["NULL"] and logits(ldz=4) == E["SHAPE"] and logits(ldz=9) == E["ALIGN"] and logits(Z=A + 4) == E["ALIGN"]
     assert top1(v=None) == E["NULL"] and top1(c=None) == E["NULL"] and top1(v=A + 1) == E["ALIGN"] and top1(off=-1) == E["RANGE"]
     assert top1(off=2**31 - 4) == E["RANGE"] and top1(wsp=None) == E["WORKSPACE"] and top1(wsb=8) == E["WORKSPACE"] and top1(wsp=A + 8) == E["ALIGN"]

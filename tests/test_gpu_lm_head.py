@@ -82,7 +82,7 @@ def test_training_step(torch, B, D, widths, limit):
     k = min(1.0, limit / float(norm))
     gamma0, W0, b0 = a.gamma.double(), a.W.double(), a.b.double()
     a.step()
-    assert abs(float(a.mean) - float(loss)) <= 1e-3 * float(loss)
+    assert abs(float(a.mean) - loss.item()) <= 1e-3 * loss.item()
     _near(a.dh, dh, "dh"), _near(a.dgamma, dgamma, "dgamma"), _near(a.dW, dW, "dW"), _near(a.db, db, "db")
     assert abs(float(a.norm) - float(norm)) <= 2e-2 * float(norm)
     # the update that was made, but for the rounding of the new weights

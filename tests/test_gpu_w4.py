@@ -115,6 +115,72 @@ def test_logits_and_top1(G, B, D, C, x_kind):
         assert np.all(want[r, at] >= want.max(1) - 2 * slack.max(1))
 
 
+# Every way of dividing the work, at sizes where it is taken: rows that stream (short and long ones), contractions shared out among waves (by every
+# number of steps), tiles of rows and classes (narrow and wide ones of every height)
+LARGE = [(1, 512, 20000), (9, 2048, 17000), (32, 1984, 17000), (1, 4224, 9000), (3, 1024, 2000), (20, 1088, 3100), (5, 2048, 1000), (64, 2048, 5000),
+         (7, 4096, 8000), (31, 4096, 500), (1, 4224, 300), (40, 8192, 2000), (20, 8256, 300), (20, 8256, 42000), (50, 576, 1000), (64, 512, 42001),
+         (40, 64, 45000), (96, 576, 83000), (100, 128, 90003), (128, 320, 83001), (250, 64, 45000)]
+
+
+def _device_layer(B, D, C, x_kind, seed):
+    """As _layer, on the device, with the 64-bit values."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    W4 = torch.randint(0, 256, (C, D // 2), device="cuda", dtype=torch.uint8, generator=gen)
+    s = torch.randint(119, 124, (C, D // 32), device="cuda", dtype=torch.uint8, generator=gen)
+    codes = torch.stack((W4 & 15, W4 >> 4), 2).reshape(C, D).long()
+    W = _dev(mx.E2M1)[codes] * torch.exp2(s.double() - 127).repeat_interleave(32, 1)
+    if x_kind == "bf16":
+        x, xs = torch.randn((B, D), device="cuda", generator=gen).bfloat16(), None
+        X = x.double()
+    else:
+        x = torch.randint(0, 256, (B, D), device="cuda", dtype=torch.uint8, generator=gen)
+        x[(x & 127) == 127] = 0
+        xs = torch.randint(116, 121, (B, D // 32), device="cuda", dtype=torch.uint8, generator=gen)
+        X = _dev(mx.E4M3)[x.long()] * torch.exp2(xs.double() - 127).repeat_interleave(32, 1)
+    return W4, s, torch.randn(C, device="cuda", generator=gen), x, xs, X, W
+
+
+@pytest.mark.parametrize("x_kind", ["bf16", "mx8"])
+@pytest.mark.parametrize("B,D,C", LARGE)
+def test_every_division_of_the_work(G, B, D, C, x_kind):
+    import torch
+    from paper_2011_09208_amd import binding as ws
+    print(f"[w4] B={B} D={D} C={C} {x_kind}", flush=True)
+    W4, s, bias, x, xs, X, W = _device_layer(B, D, C, x_kind, B + D + C)
+    want = X @ W.T + bias.double()
+    slack = (D / 32 + 32 + 16) * 2.0 ** -23 * (X.abs() @ W.abs().T + 4.0)                # as _slack
+    Z = G.Guarded(B, C, torch.float32, pad_cols=(-C) % 4 + 4)
+    ws.split_fc_w4_logits(x, xs, W4, s, bias, Z.t)
+    torch.cuda.synchronize()
+    assert Z.intact_outside_payload()
+    assert bool(((Z.t.double() - want).abs() <= slack).all())
+    top, cls, work = G.Guarded(1, B, torch.float32), G.Guarded(1, B, torch.int32), G.Guarded(1, ws.w4_top1_workspace_bytes(B, C), torch.uint8)
+    ws.split_fc_w4_top1(x, xs, W4, s, bias, 7, top.vec(), cls.vec(), work.vec())
+    torch.cuda.synchronize()
+    assert top.intact_outside_payload() and cls.intact_outside_payload() and work.intact_outside_payload()
+    at = (cls.vec().long() - 7)[:, None]
+    assert bool(((at >= 0) & (at < C)).all())
+    assert bool(((top.vec().double()[:, None] - want.gather(1, at)).abs() <= slack.gather(1, at)).all())
+    assert bool((want.gather(1, at)[:, 0] >= want.max(1).values - 2 * slack.max(1).values).all())
+
+
+def test_as_many_rows_as_there_may_be(G):
+    """2^20 rows against several groups of classes; every row is one of 64 that come again and again."""
+    import torch
+    from paper_2011_09208_amd import binding as ws
+    B, D, C = 1 << 20, 64, 17000
+    W4, s, bias, x, _, X, W = _device_layer(64, D, C, "bf16", 3)
+    want = X @ W.T + bias.double()
+    top, cls = torch.empty(B, device="cuda"), torch.empty(B, device="cuda", dtype=torch.int32)
+    work = torch.empty(ws.w4_top1_workspace_bytes(B, C), device="cuda", dtype=torch.uint8)
+    ws.split_fc_w4_top1(x.repeat(B // 64, 1), None, W4, s, bias, 0, top, cls, work)
+    at = cls[:64].long()[:, None]
+    slack = (D / 32 + 32 + 16) * 2.0 ** -23 * (X.abs() @ W.abs().T + 4.0)
+    assert bool((want.gather(1, at)[:, 0] >= want.max(1).values - 2 * slack.max(1).values).all())
+    assert torch.equal(cls.view(-1, 64), cls[:64].expand(B // 64, 64)) and torch.equal(top.view(-1, 64), top[:64].expand(B // 64, 64))
+
+
 def test_pitches_and_slices_of_a_packed_layer(G):
     """A slice of the rows of the packed layer is the shard; pitched codes, scales and features."""
     import torch
