@@ -285,12 +285,12 @@ __device__ __forceinline__ void w4_report(const W4Args& a, float (&best)[NT], in
 // A wave takes CT x 16 classes and 16 NT rows, a workgroup WAVES waves along the classes; tile c of all waves makes WAVES x 16 neighbouring classes.
 // A step of the rows' features is in LDS, the next one on its way to the other half, and so are the next codes.  A step takes 2.2 us with 64
 // rows, most of it the way of its codes: load, exchange between lanes, conversion, product; with 256 rows the matrix instructions and LDS, from which
-// every wave reads every feature fragment, for CT products each.  200 x 1088 x 50 001: 39.8 us, 128 x 2048 x 100 000: 65 (800 TFLOP/s), 256: 122 (860).
+// every wave reads every feature fragment, for CT products each.  200 x 1088 x 50 001: 38.2 us, 128 x 2048 x 100 000: 65 (800 TFLOP/s), 256: 117 (900).
 // Up to 64 rows CT = 2 leaves registers for two workgroups on a compute unit, which fill each other's pauses (64 x 256 x 100 000 classes 15.2 us,
 // CT = 4 17.8); with more rows CT = 4 halves what is read from LDS for a product.
 //
 // Tried and slower: the codes of two steps on their way (64 x 2048 x 100 000 classes 48.8 us, now 47.4); the scales of 16 steps through LDS
-// (a step of 64 rows is 15 % faster, but the start costs 7 us: 200 x 1088 x 50 001 49.6 us, now 39.8).
+// (a step of 64 rows is 15 % faster, but the start costs 7 us: 200 x 1088 x 50 001 49.6 us, otherwise 39.8).
 //
 // Logits leave through LDS, one c after the other, in a loop that is not unrolled: straight from the accumulators every one of the CT NT 4 stores
 // and bounds checks is code of its own, 10 KiB that each launch fetches anew (128 rows x 256 features x 100 000 classes 28.6 us).
@@ -797,13 +797,18 @@ static W4Plan w4_plan(int B, int D, int C, bool top1) {
         p.ring = steps > 32 && tiles <= 1024 ? 2 : 1;
     } else {
         const int row_tiles = (B + 15) / 16;
-        auto padded = [&](int nt) { return (row_tiles + nt - 1) / nt * nt; };
-        p.NT = row_tiles <= 2 ? 2 : row_tiles <= 4 || top1 ? 4 : padded(6) < padded(8) ? 6 : 8;      // the rows' candidates take registers, too
-        const int wide = p.NT <= 4 ? 16 : 32;
-        p.wide = (tiles + wide - 1) / wide * (padded(p.NT) / p.NT) >= 160;
-        if (!p.wide && p.NT > 4) p.NT = 4;
-        const int at_once = p.wide ? wide : 8;
-        p.groups = (int)((tiles + at_once - 1) / at_once);
+        // Blocks of rows of one height, up to 8 tiles of 16 with CT = 4 tiles of classes, up to 4 with CT = 2; eight waves to a workgroup, or four.  The
+        // tall ones for logits only (the arg-max's candidates take registers, too: 256 x 2048 x 100 000 153 us with 6 tiles, 134 with 4), and
+        // whatever is larger only while there are workgroups for most compute units (80 x 2048 x 50 000: 45 us with four waves, 42 with eight).
+        auto shape = [&](int most_rows, int classes) {
+            const int blocks = (row_tiles + most_rows - 1) / most_rows;
+            p.NT = (row_tiles + blocks - 1) / blocks;
+            p.groups = (int)((tiles + classes - 1) / classes);
+            return (int64_t)p.groups * blocks >= 160;
+        };
+        p.wide = (!top1 && row_tiles > 4 && shape(8, 32)) || shape(4, 16);
+        if (!p.wide) shape(4, 8);
+        if (p.NT <= 4) p.NT = p.NT <= 2 ? 2 : 4;
     }
     return p;
 }
@@ -862,9 +867,15 @@ static void launch_w4_type(const W4Args& a, hipStream_t s) {
     switch (p.NT) {
         case 2: return launch_w4_tiles<2, 2, 8, MX, TOP1>(a, p, s);
         case 4: return launch_w4_tiles<4, 2, 8, MX, TOP1>(a, p, s);
-        case 6: if constexpr (!TOP1) return launch_w4_tiles<6, 4, 8, MX, false>(a, p, s);
-        default: if constexpr (!TOP1) return launch_w4_tiles<8, 4, 8, MX, false>(a, p, s);
+        default: break;
     }
+    if constexpr (!TOP1)
+        switch (p.NT) {
+            case 5: return launch_w4_tiles<5, 4, 8, MX, false>(a, p, s);
+            case 6: return launch_w4_tiles<6, 4, 8, MX, false>(a, p, s);
+            case 7: return launch_w4_tiles<7, 4, 8, MX, false>(a, p, s);
+            default: return launch_w4_tiles<8, 4, 8, MX, false>(a, p, s);
+        }
 }
 
 template <bool TOP1>
