@@ -387,8 +387,8 @@ int ws_probe_gemm(const void* A, int64_t lda, const void* B, int64_t ldb, int32_
 
 /* Optional per-kernel timing, for benchmarks (not part of the paper's method; host-side state,
  * not thread safe).  ws_profile_enable(n) creates a pool of n event pairs (n <= 0 switches
- * timing off and frees the pool); while the pool lasts, every kernel the library launches is
- * bracketed by two events recorded on the launch stream.  ws_profile_reset() starts a new
+ * timing off and frees the pool); while the pool lasts, every launch of a kernel that ws_profile_kernel_name
+ * names is bracketed by two events recorded on the launch stream.  ws_profile_reset() starts a new
  * measurement.  ws_profile_pause(1) lets launches go untimed until ws_profile_pause(0) (a benchmark can
  * time the kernels of every n-th step only, so that the event records perturb the step time less).
  * ws_profile_read() waits for the recorded events of one kernel (indices

@@ -151,9 +151,13 @@ def _ptr(t):
 try:
     from torch._C import _cuda_getCurrentRawStream, _cuda_getDevice
 
+    _device = _cuda_getDevice
+
     def _stream():
         return _cuda_getCurrentRawStream(_cuda_getDevice())
 except ImportError:                      # PyTorch's own names, which a build without a GPU lacks: the host functions work there, too
+    _device = torch.cuda.current_device
+
     def _stream():
         return torch.cuda.current_stream().cuda_stream
 
@@ -357,10 +361,10 @@ _BYTE_TYPES = (torch.uint8, torch.float8_e4m3fn)
 
 
 def _matrix(t, shape, dtype):
-    """(address, row pitch) of a device tensor of this shape whose rows are contiguous; (None, 0) for no tensor."""
+    """(address, row pitch) of a tensor on the current device, of this shape and with contiguous rows; (None, 0) for no tensor."""
     if t is None:
         return None, 0
-    assert t.dtype is dtype and t.shape == shape and t.is_cuda
+    assert t.dtype is dtype and t.shape == shape and 0 <= t.get_device() == _device()
     ld, unit = t.stride()
     if unit != 1 or ld < shape[1]:                         # a single row or column may have any stride
         assert (unit == 1 or shape[1] == 1) and (ld >= shape[1] or shape[0] == 1)
@@ -376,8 +380,16 @@ def _bytes_matrix(t, shape):
 def _vector(t, n, dtype):
     if t is None:
         return None
-    assert t.dtype is dtype and t.shape == (n,) and t.is_contiguous() and t.is_cuda
+    assert t.dtype is dtype and t.shape == (n,) and t.is_contiguous() and 0 <= t.get_device() == _device()
     return t.data_ptr()
+
+
+def _scratch(t):
+    """(address, bytes) of a workspace."""
+    if t is None:
+        return None, 0
+    assert t.is_contiguous() and 0 <= t.get_device() == _device()
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _stream_type(a, b):
@@ -417,7 +429,7 @@ def rms_norm_bwd(dY, h, dres, gamma, rstd, dh, dgamma, workspace):
     kind = h.dtype
     _check(lib.ws_rms_norm_bwd(*_matrix(dY, shape, _FP32), *_matrix(h, shape, kind), *_matrix(dres, shape, kind), _STREAM_TYPES[kind],
                                _vector(gamma, D, _FP32), _vector(rstd, B, _FP32), B, D, *_matrix(dh, shape, kind), _vector(dgamma, D, _FP32),
-                               _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+                               *_scratch(workspace), _stream()))
 
 
 def quantize_mx4(W, W4, W_scales):
@@ -451,7 +463,7 @@ def split_fc_w4_top1(X, X_scales, W4, W_scales, b_shard, class_offset, top_logit
     """top_logit fp32 [B], top_class int32 [B] <- the shard's best class per row; inputs as split_fc_w4_logits."""
     a = _w4_args(X, X_scales, W4, W_scales, b_shard)
     _check(lib.ws_split_fc_w4_top1(*a, int(class_offset), _vector(top_logit, a[9], _FP32), _vector(top_class, a[9], _I32),
-                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
+                                   *_scratch(workspace), _stream()))
 
 
 _ONES = array.array("q", [1]) * 4096
@@ -466,7 +478,8 @@ class grad_table:
         self.n = n = len(tensors)
         T = torch.Tensor
         elem_bytes = array.array("i", map(_STREAM_TYPES.__getitem__, map(attrgetter("dtype"), tensors)))
-        assert all(map(attrgetter("is_cuda"), tensors))
+        places = set(map(T.get_device, tensors))
+        assert not places or places == {max(0, *places)} == {_device()}
         if not by_rows and n <= len(_ONES) and all(map(T.is_contiguous, tensors)):       # each one long row
             rows = _ONES
             lds = cols = array.array("q", map(T.numel, tensors))
@@ -502,8 +515,7 @@ def grad_workspace_bytes(n):
 def grad_sumsq(grads, sumsq, workspace):
     """sumsq fp64 [1] <- the sum of the squares of all gradients (tensors, or their grad_table)."""
     g = _table(grads)
-    _check(lib.ws_grad_sumsq(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, 1, torch.float64), _ptr(workspace),
-                             workspace.numel() * workspace.element_size(), _stream()))
+    _check(lib.ws_grad_sumsq(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, 1, _F64), *_scratch(workspace), _stream()))
 
 
 def grad_clip(grads, sumsq, max_norm, norm=None):
@@ -521,7 +533,7 @@ def grad_clip_sgd(params, grads, sumsq, max_norm, lr, norm=None):
     if p.extents != g.extents:                             # one of a pair has a pitch: both are described by their rows
         p, g = grad_table(p.tensors, True), grad_table(g.tensors, True)
         assert p.extents == g.extents
-    _check(lib.ws_grad_clip_sgd(p.data, p.lds, p.bytes, g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, torch.float64), S,
+    _check(lib.ws_grad_clip_sgd(p.data, p.lds, p.bytes, g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, _F64), S,
                                 float(max_norm), float(lr), _vector(norm, 1, torch.float32), _stream()))
 
 

@@ -305,14 +305,26 @@ static int check_norm(const void* x, int64_t ldx, const void* residual, int64_t 
     return WS_OK;
 }
 
+// A launch counts its threads with 32 bits, up to 1024 for a row: more rows go slice by slice.
+constexpr int NORM_SLICE = 1 << 21;
+
 template <bool FP32, bool MX>
-static void launch_norm(const NormArgs& a, hipStream_t s) {
-    if (a.D <= 512) hipLaunchKernelGGL((rms_norm_fwd<64, 1, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
-    else if (a.D <= 1024) hipLaunchKernelGGL((rms_norm_fwd<64, 2, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
-    else if (a.D <= 2048) hipLaunchKernelGGL((rms_norm_fwd<64, 4, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
-    else if (a.D <= 4096) hipLaunchKernelGGL((rms_norm_fwd<256, 2, FP32, MX>), dim3(a.B), dim3(256), 0, s, a);
-    else if (a.D <= 8192) hipLaunchKernelGGL((rms_norm_fwd<256, 4, FP32, MX>), dim3(a.B), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((rms_norm_fwd<1024, 2, FP32, MX>), dim3(a.B), dim3(1024), 0, s, a);
+static void launch_norm(NormArgs a, hipStream_t s) {
+    for (int left = a.B; left > 0; left -= NORM_SLICE) {
+        a.B = left < NORM_SLICE ? left : NORM_SLICE;
+        if (a.D <= 512) hipLaunchKernelGGL((rms_norm_fwd<64, 1, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
+        else if (a.D <= 1024) hipLaunchKernelGGL((rms_norm_fwd<64, 2, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
+        else if (a.D <= 2048) hipLaunchKernelGGL((rms_norm_fwd<64, 4, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
+        else if (a.D <= 4096) hipLaunchKernelGGL((rms_norm_fwd<256, 2, FP32, MX>), dim3(a.B), dim3(256), 0, s, a);
+        else if (a.D <= 8192) hipLaunchKernelGGL((rms_norm_fwd<256, 4, FP32, MX>), dim3(a.B), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((rms_norm_fwd<1024, 2, FP32, MX>), dim3(a.B), dim3(1024), 0, s, a);
+        a.x += a.B * a.ldx;
+        if (a.res) a.res = static_cast<const char*>(a.res) + a.B * a.ldr * (FP32 ? 4 : 2);
+        if (a.h) a.h = static_cast<char*>(a.h) + a.B * a.ldh * (FP32 ? 4 : 2);
+        a.y = static_cast<char*>(a.y) + a.B * a.ldy * (MX ? 1 : 2);
+        if (MX) a.scales += a.B * a.lds;
+        if (a.rstd) a.rstd += a.B;
+    }
 }
 
 template <bool FP32>

@@ -122,6 +122,47 @@ def test_rows_with_infinities_and_nans(G):
 
 
 @pytest.mark.parametrize("stream", ["bf16", "fp32"])
+def test_more_rows_than_a_launch_takes(G, stream):
+    """2^21 + 70 rows, 64 that come again and again: the result of a row does not depend on where it is."""
+    import torch
+    from paper_2011_09208_amd import binding as ws
+    B, D = (1 << 21) + 70, 64
+    x, res, gamma, dt = _inputs(64, D, stream, 12)
+    many = lambda t: t.repeat(B // 64 + 1, *[1] * (t.dim() - 1))[:B].contiguous()        # noqa: E731
+    h, y, rstd = torch.empty((64, D), device="cuda", dtype=dt), torch.empty_like(x), torch.empty(64, device="cuda")
+    ws.rms_norm_fwd(x, res, gamma, 1e-6, h, y, rstd)
+    H, Y, R = torch.empty((B, D), device="cuda", dtype=dt), torch.empty((B, D), device="cuda", dtype=torch.bfloat16), torch.empty(B, device="cuda")
+    ws.rms_norm_fwd(many(x), many(res), gamma, 1e-6, H, Y, R)
+    assert torch.equal(H, many(h)) and torch.equal(Y, many(y)) and torch.equal(R, many(rstd))
+    q, s = torch.empty((64, D), device="cuda", dtype=torch.uint8), torch.empty((64, 2), device="cuda", dtype=torch.uint8)
+    ws.rms_norm_fwd_mx8(x, res, gamma, 1e-6, None, q, s, None)
+    Q, S = torch.empty((B, D), device="cuda", dtype=torch.uint8), torch.empty((B, 2), device="cuda", dtype=torch.uint8)
+    ws.rms_norm_fwd_mx8(many(x), many(res), gamma, 1e-6, H, Q, S, R)
+    assert torch.equal(Q, many(q)) and torch.equal(S, many(s)) and torch.equal(H, many(h)) and torch.equal(R, many(rstd))
+
+
+def test_tensors_of_another_device_are_refused(G, monkeypatch):
+    import torch
+    from paper_2011_09208_amd import binding as ws
+    x, res, gamma, _ = _inputs(4, 64, "bf16", 1)
+    y, work = torch.empty_like(x), torch.empty(1 << 16, device="cuda", dtype=torch.uint8)
+    sumsq = torch.empty(1, device="cuda", dtype=torch.float64)
+    ws.rms_norm_fwd(x, res, gamma, 1e-6, None, y, None)
+    ws.grad_sumsq([x, gamma], sumsq, work)
+    torch.cuda.synchronize()
+    table = ws.grad_table([x, gamma])
+    monkeypatch.setattr(ws, "_device", lambda: 1)
+    for call in (lambda: ws.rms_norm_fwd(x, res, gamma, 1e-6, None, y, None), lambda: ws.grad_table([x]), lambda: ws.grad_sumsq(table, sumsq, work),
+                 lambda: ws.quantize_mx4(x, torch.empty((4, 32), device="cuda", dtype=torch.uint8), torch.empty((4, 2), device="cuda", dtype=torch.uint8)),
+                 lambda: ws.grad_clip(table, sumsq, 1.0)):
+        with pytest.raises(AssertionError):
+            call()
+    monkeypatch.undo()
+    with pytest.raises(AssertionError):
+        ws.grad_table([x, gamma.cpu()])
+
+
+@pytest.mark.parametrize("stream", ["bf16", "fp32"])
 @pytest.mark.parametrize("B,D", SIZES + [(4099, 64), (2500, 2048)])
 def test_way_back(G, B, D, stream):
     import torch
