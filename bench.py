@@ -359,6 +359,34 @@ def measure_extras(args, result, ws, torch, dev, X, W, y, B, D, C, work, lse, lo
         }
         del zparts
 
+    # Around the layer in a language model: norm and its way back for this batch, the packed layer for one token and for 32, the norm of the
+    # layer's gradients and the clipped update.  lr = 0 keeps W as it is.
+    if args.workload == "headline":
+        gamma, rstd, dY, dgamma = torch.ones(D, device=dev), torch.empty(B, device=dev), torch.randn((B, D), device=dev), torch.empty(D, device=dev)
+        h, Xn, dh = torch.empty_like(X), torch.empty_like(X), torch.empty_like(X)
+        W4, Ws = (torch.empty((C, n), device=dev, dtype=torch.uint8) for n in (D // 2, D // 32))
+        dW, Z = torch.randn((C, D), device=dev).to(torch.bfloat16), torch.empty((32, C), device=dev)
+        top, cls, sumsq, norm = torch.empty(1, device=dev), torch.empty(1, device=dev, dtype=torch.int32), torch.empty(1, device=dev, dtype=torch.float64), torch.empty(1, device=dev)
+        aux = torch.empty(max(ws.rms_norm_bwd_workspace_bytes(B, D), ws.w4_top1_workspace_bytes(1, C), ws.grad_workspace_bytes(1)), device=dev, dtype=torch.uint8)
+        grads, params = ws.grad_table([dW]), ws.grad_table([W])
+
+        def clipped_update():
+            ws.grad_sumsq(grads, sumsq, aux)
+            ws.grad_clip_sgd(params, grads, sumsq, 1.0, 0.0, norm)
+
+        packed = C * (D / 2 + D / 32)
+        around = {}
+        for name, n_bytes, fn in (
+                ("rms_norm_fwd", 8.0 * B * D, lambda: ws.rms_norm_fwd(X, X, gamma, 1e-6, h, Xn, rstd)),
+                ("rms_norm_bwd", 8.0 * B * D, lambda: ws.rms_norm_bwd(dY, h, None, gamma, rstd, dh, dgamma, aux)),
+                ("quantize_mx4", 2.0 * C * D + packed, lambda: ws.quantize_mx4(W, W4, Ws)),
+                ("split_fc_w4_top1, 1 token", packed, lambda: ws.split_fc_w4_top1(X[:1], None, W4, Ws, None, 0, top, cls, aux)),
+                ("split_fc_w4_logits, 32 tokens", packed + 128.0 * C, lambda: ws.split_fc_w4_logits(X[:32], None, W4, Ws, None, Z)),
+                ("grad_sumsq + grad_clip_sgd", 8.0 * C * D, clipped_update)):
+            us = timed(fn, 20)
+            around[name] = {"us": round(us, 2), "bytes": n_bytes, "GB/s": round(n_bytes / us / 1e3, 1)}
+        result["around_the_layer"] = around
+
 
 def trace_dw(ws, torch, np, step, workload, B, D, shards):
     """Where the cycles of a workgroup of bwd_dw go, the dW kernel with one workgroup per tile, which is that of the

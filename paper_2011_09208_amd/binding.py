@@ -360,11 +360,19 @@ _STREAM_TYPES = {_BF16: 2, _FP32: 4}
 _BYTE_TYPES = (torch.uint8, torch.float8_e4m3fn)
 
 
-def _matrix(t, shape, dtype):
-    """(address, row pitch) of a tensor on the current device, of this shape and with contiguous rows; (None, 0) for no tensor."""
+# A call of the norm spends 3.3 us in its checks and 3.7 in the library: the current device is asked for once.
+def _here(t):
+    """The current device, where the tensor has to be."""
+    dev = t.get_device()
+    assert 0 <= dev == _device()
+    return dev
+
+
+def _matrix(t, shape, dtype, dev):
+    """(address, row pitch) of a tensor on this device, of this shape and with contiguous rows; (None, 0) for no tensor."""
     if t is None:
         return None, 0
-    assert t.dtype is dtype and t.shape == shape and 0 <= t.get_device() == _device()
+    assert t.dtype is dtype and t.shape == shape and t.get_device() == dev
     ld, unit = t.stride()
     if unit != 1 or ld < shape[1]:                         # a single row or column may have any stride
         assert (unit == 1 or shape[1] == 1) and (ld >= shape[1] or shape[0] == 1)
@@ -372,23 +380,23 @@ def _matrix(t, shape, dtype):
     return t.data_ptr(), ld
 
 
-def _bytes_matrix(t, shape):
+def _bytes_matrix(t, shape, dev):
     """_matrix of 8-bit values of either type."""
-    return _matrix(t, shape, _BYTE_TYPES[1] if t.dtype is _BYTE_TYPES[1] else _BYTE_TYPES[0])
+    return _matrix(t, shape, _BYTE_TYPES[1] if t.dtype is _BYTE_TYPES[1] else _BYTE_TYPES[0], dev)
 
 
-def _vector(t, n, dtype):
+def _vector(t, n, dtype, dev):
     if t is None:
         return None
-    assert t.dtype is dtype and t.shape == (n,) and t.is_contiguous() and 0 <= t.get_device() == _device()
+    assert t.dtype is dtype and t.shape == (n,) and t.is_contiguous() and t.get_device() == dev
     return t.data_ptr()
 
 
-def _scratch(t):
+def _scratch(t, dev):
     """(address, bytes) of a workspace."""
     if t is None:
         return None, 0
-    assert t.is_contiguous() and 0 <= t.get_device() == _device()
+    assert t.is_contiguous() and t.get_device() == dev
     return t.data_ptr(), t.numel() * t.element_size()
 
 
@@ -400,21 +408,21 @@ def _stream_type(a, b):
 def rms_norm_fwd(x, residual, gamma, eps, h, y, rstd):
     """h = residual + x, y = h * rstd * gamma.  x, y bf16 [B, D]; residual, h bf16 or fp32 [B, D] or None; gamma fp32 [D];
     rstd fp32 [B] or None.  h may be residual itself."""
-    shape = x.shape
+    dev, shape = _here(x), x.shape
     B, D = shape
     kind = _stream_type(residual, h)
-    _check(lib.ws_rms_norm_fwd(*_matrix(x, shape, _BF16), *_matrix(residual, shape, kind), _STREAM_TYPES[kind], _vector(gamma, D, _FP32),
-                               eps, B, D, *_matrix(h, shape, kind), *_matrix(y, shape, _BF16), _vector(rstd, B, _FP32), _stream()))
+    _check(lib.ws_rms_norm_fwd(*_matrix(x, shape, _BF16, dev), *_matrix(residual, shape, kind, dev), _STREAM_TYPES[kind], _vector(gamma, D, _FP32, dev),
+                               eps, B, D, *_matrix(h, shape, kind, dev), *_matrix(y, shape, _BF16, dev), _vector(rstd, B, _FP32, dev), _stream()))
 
 
 def rms_norm_fwd_mx8(x, residual, gamma, eps, h, y, y_scales, rstd):
     """rms_norm_fwd with y in 8 bits: y uint8 or float8_e4m3fn [B, D], y_scales uint8 [B, D / 32]."""
-    shape = x.shape
+    dev, shape = _here(x), x.shape
     B, D = shape
     kind = _stream_type(residual, h)
-    _check(lib.ws_rms_norm_fwd_mx8(*_matrix(x, shape, _BF16), *_matrix(residual, shape, kind), _STREAM_TYPES[kind], _vector(gamma, D, _FP32),
-                                   eps, B, D, *_matrix(h, shape, kind), *_bytes_matrix(y, shape), *_matrix(y_scales, (B, D // 32), torch.uint8),
-                                   _vector(rstd, B, _FP32), _stream()))
+    _check(lib.ws_rms_norm_fwd_mx8(*_matrix(x, shape, _BF16, dev), *_matrix(residual, shape, kind, dev), _STREAM_TYPES[kind], _vector(gamma, D, _FP32, dev),
+                                   eps, B, D, *_matrix(h, shape, kind, dev), *_bytes_matrix(y, shape, dev), *_matrix(y_scales, (B, D // 32), torch.uint8, dev),
+                                   _vector(rstd, B, _FP32, dev), _stream()))
 
 
 def rms_norm_bwd_workspace_bytes(B, D):
@@ -424,35 +432,36 @@ def rms_norm_bwd_workspace_bytes(B, D):
 def rms_norm_bwd(dY, h, dres, gamma, rstd, dh, dgamma, workspace):
     """dY fp32 [B, D]; h, dh and dres (or None) bf16 or fp32 [B, D]; gamma fp32 [D]; rstd fp32 [B]; dgamma fp32 [D], or None: then
     workspace may be None, else it has rms_norm_bwd_workspace_bytes.  dh may be dres itself."""
-    shape = dY.shape
+    dev, shape = _here(dY), dY.shape
     B, D = shape
     kind = h.dtype
-    _check(lib.ws_rms_norm_bwd(*_matrix(dY, shape, _FP32), *_matrix(h, shape, kind), *_matrix(dres, shape, kind), _STREAM_TYPES[kind],
-                               _vector(gamma, D, _FP32), _vector(rstd, B, _FP32), B, D, *_matrix(dh, shape, kind), _vector(dgamma, D, _FP32),
-                               *_scratch(workspace), _stream()))
+    _check(lib.ws_rms_norm_bwd(*_matrix(dY, shape, _FP32, dev), *_matrix(h, shape, kind, dev), *_matrix(dres, shape, kind, dev), _STREAM_TYPES[kind],
+                               _vector(gamma, D, _FP32, dev), _vector(rstd, B, _FP32, dev), B, D, *_matrix(dh, shape, kind, dev), _vector(dgamma, D, _FP32, dev),
+                               *_scratch(workspace, dev), _stream()))
 
 
 def quantize_mx4(W, W4, W_scales):
     """W bf16 [C, D] -> W4 uint8 [C, D / 2] (two codes to a byte, the first in the low bits), W_scales uint8 [C, D / 32]."""
-    C, D = W.shape
-    _check(lib.ws_quantize_mx4(*_matrix(W, W.shape, _BF16), C, D, *_matrix(W4, (C, D // 2), torch.uint8),
-                               *_matrix(W_scales, (C, D // 32), torch.uint8), _stream()))
+    dev, (C, D) = _here(W), W.shape
+    _check(lib.ws_quantize_mx4(*_matrix(W, W.shape, _BF16, dev), C, D, *_matrix(W4, (C, D // 2), torch.uint8, dev),
+                               *_matrix(W_scales, (C, D // 32), torch.uint8, dev), _stream()))
 
 
-def _w4_args(X, X_scales, W4, W_scales, b_shard):
+def _w4_args(X, X_scales, W4, W_scales, b_shard, dev):
     shape = X.shape
     B, D = shape
     C = W4.shape[0]
-    x = _matrix(X, shape, _BF16) if X_scales is None else _bytes_matrix(X, shape)
-    return (*x, *_matrix(X_scales, (B, D // 32), torch.uint8), *_matrix(W4, (C, D // 2), torch.uint8),
-            *_matrix(W_scales, (C, D // 32), torch.uint8), _vector(b_shard, C, _FP32), B, D, C)
+    x = _matrix(X, shape, _BF16, dev) if X_scales is None else _bytes_matrix(X, shape, dev)
+    return (*x, *_matrix(X_scales, (B, D // 32), torch.uint8, dev), *_matrix(W4, (C, D // 2), torch.uint8, dev),
+            *_matrix(W_scales, (C, D // 32), torch.uint8, dev), _vector(b_shard, C, _FP32, dev), B, D, C)
 
 
 def split_fc_w4_logits(X, X_scales, W4, W_scales, b_shard, Z):
     """Z fp32 [B, C_shard] (row pitch a multiple of 4) <- X . W^T + b.  X bf16 [B, D] with X_scales None, or uint8 / float8_e4m3fn with
     X_scales uint8 [B, D / 32]; W4, W_scales as quantize_mx4 leaves them; b_shard fp32 [C_shard] or None."""
-    a = _w4_args(X, X_scales, W4, W_scales, b_shard)
-    _check(lib.ws_split_fc_w4_logits(*a, *_matrix(Z, (a[9], a[11]), _FP32), _stream()))
+    dev = _here(X)
+    a = _w4_args(X, X_scales, W4, W_scales, b_shard, dev)
+    _check(lib.ws_split_fc_w4_logits(*a, *_matrix(Z, (a[9], a[11]), _FP32, dev), _stream()))
 
 
 def w4_top1_workspace_bytes(B, C_shard):
@@ -461,9 +470,10 @@ def w4_top1_workspace_bytes(B, C_shard):
 
 def split_fc_w4_top1(X, X_scales, W4, W_scales, b_shard, class_offset, top_logit, top_class, workspace):
     """top_logit fp32 [B], top_class int32 [B] <- the shard's best class per row; inputs as split_fc_w4_logits."""
-    a = _w4_args(X, X_scales, W4, W_scales, b_shard)
-    _check(lib.ws_split_fc_w4_top1(*a, int(class_offset), _vector(top_logit, a[9], _FP32), _vector(top_class, a[9], _I32),
-                                   *_scratch(workspace), _stream()))
+    dev = _here(X)
+    a = _w4_args(X, X_scales, W4, W_scales, b_shard, dev)
+    _check(lib.ws_split_fc_w4_top1(*a, int(class_offset), _vector(top_logit, a[9], _FP32, dev), _vector(top_class, a[9], _I32, dev),
+                                   *_scratch(workspace, dev), _stream()))
 
 
 _ONES = array.array("q", [1]) * 4096
@@ -479,7 +489,8 @@ class grad_table:
         T = torch.Tensor
         elem_bytes = array.array("i", map(_STREAM_TYPES.__getitem__, map(attrgetter("dtype"), tensors)))
         places = set(map(T.get_device, tensors))
-        assert not places or places == {max(0, *places)} == {_device()}
+        self.device = _here(tensors[0]) if tensors else None
+        assert len(places) <= 1
         if not by_rows and n <= len(_ONES) and all(map(T.is_contiguous, tensors)):       # each one long row
             rows = _ONES
             lds = cols = array.array("q", map(T.numel, tensors))
@@ -504,8 +515,10 @@ class grad_table:
         return self._arrays[1][:self.n], self._arrays[2]
 
 
-def _table(tensors):
-    return tensors if isinstance(tensors, grad_table) else grad_table(tensors)
+def _table(tensors, dev):
+    table = tensors if isinstance(tensors, grad_table) else grad_table(tensors)
+    assert table.device in (dev, None)
+    return table
 
 
 def grad_workspace_bytes(n):
@@ -514,27 +527,28 @@ def grad_workspace_bytes(n):
 
 def grad_sumsq(grads, sumsq, workspace):
     """sumsq fp64 [1] <- the sum of the squares of all gradients (tensors, or their grad_table)."""
-    g = _table(grads)
-    _check(lib.ws_grad_sumsq(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, 1, _F64), *_scratch(workspace), _stream()))
+    dev = _here(sumsq)
+    g = _table(grads, dev)
+    _check(lib.ws_grad_sumsq(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, 1, _F64, dev), *_scratch(workspace, dev), _stream()))
 
 
 def grad_clip(grads, sumsq, max_norm, norm=None):
     """Scales the gradients in place by min(1, max_norm / norm), norm = sqrt(sum of sumsq fp64 [S]); norm fp32 [1] or None."""
-    g = _table(grads)
-    S = sumsq.numel()
-    _check(lib.ws_grad_clip(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, _F64), S, float(max_norm),
-                            _vector(norm, 1, torch.float32), _stream()))
+    S, dev = sumsq.numel(), _here(sumsq)
+    g = _table(grads, dev)
+    _check(lib.ws_grad_clip(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, _F64, dev), S, float(max_norm),
+                            _vector(norm, 1, torch.float32, dev), _stream()))
 
 
 def grad_clip_sgd(params, grads, sumsq, max_norm, lr, norm=None):
     """params[i] <- params[i] - lr * k * grads[i] with grad_clip's factor k; the gradients are left as they are."""
-    p, g = _table(params), _table(grads)
-    S = sumsq.numel()
+    S, dev = sumsq.numel(), _here(sumsq)
+    p, g = _table(params, dev), _table(grads, dev)
     if p.extents != g.extents:                             # one of a pair has a pitch: both are described by their rows
         p, g = grad_table(p.tensors, True), grad_table(g.tensors, True)
         assert p.extents == g.extents
-    _check(lib.ws_grad_clip_sgd(p.data, p.lds, p.bytes, g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, _F64), S,
-                                float(max_norm), float(lr), _vector(norm, 1, torch.float32), _stream()))
+    _check(lib.ws_grad_clip_sgd(p.data, p.lds, p.bytes, g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, _F64, dev), S,
+                                float(max_norm), float(lr), _vector(norm, 1, torch.float32, dev), _stream()))
 
 
 def sp2_partial_logits(X_slice, W_slice, Z_partial):

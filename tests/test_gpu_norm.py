@@ -158,6 +158,9 @@ def test_tensors_of_another_device_are_refused(G, monkeypatch):
         with pytest.raises(AssertionError):
             call()
     monkeypatch.undo()
+    table.device = 1                                      # built while another device was the current one
+    with pytest.raises(AssertionError):
+        ws.grad_sumsq(table, sumsq, work)
     with pytest.raises(AssertionError):
         ws.grad_table([x, gamma.cpu()])
 
