@@ -487,13 +487,17 @@ class grad_table:
         self.tensors = tensors = list(tensors)
         self.n = n = len(tensors)
         T = torch.Tensor
-        elem_bytes = array.array("i", map(_STREAM_TYPES.__getitem__, map(attrgetter("dtype"), tensors)))
+        kinds = list(map(attrgetter("dtype"), tensors))
+        if len(set(kinds)) == 1:
+            elem_bytes = array.array("i", [_STREAM_TYPES[kinds[0]]]) * n
+        else:
+            elem_bytes = array.array("i", list(map(_STREAM_TYPES.__getitem__, kinds)))
         places = set(map(T.get_device, tensors))
         self.device = _here(tensors[0]) if tensors else None
         assert len(places) <= 1
         if not by_rows and n <= len(_ONES) and all(map(T.is_contiguous, tensors)):       # each one long row
             rows = _ONES
-            lds = cols = array.array("q", map(T.numel, tensors))
+            lds = cols = array.array("q", list(map(T.numel, tensors)))
         else:
             rows, cols, lds = [array.array("q") for _ in range(3)]
             for t in tensors:
@@ -506,7 +510,7 @@ class grad_table:
                 rows.append(r)
                 cols.append(c)
                 lds.append(ld if r > 1 else c)
-        data = array.array("q", map(T.data_ptr, tensors))
+        data = array.array("q", list(map(T.data_ptr, tensors)))
         self._arrays = (data, rows, cols, lds, elem_bytes)                   # they own what the addresses point at
         self.data, self.rows, self.cols, self.lds, self.bytes = [a.buffer_info()[0] for a in self._arrays]
 
