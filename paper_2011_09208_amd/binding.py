@@ -119,6 +119,7 @@ lib.ws_grad_clip_sgd.argtypes = [_p, _p, _p, _p, _p, _p, _p, _p, _i32, _p, _i32,
 
 STATIC_SCRATCH_BYTES = 16 << 20
 RMS_NORM_MAX_D = 16384
+W4_MAX_CLASSES = (1 << 30) - 65536
 
 EXPORTS = ["ws_status_string", "ws_version", "ws_fwd_workspace_bytes", "ws_split_fc_fwd", "ws_split_fc_fwd_static",
            "ws_combine_partials", "ws_bwd_workspace_bytes", "ws_split_fc_bwd", "ws_split_fc_bwd_sgd", "ws_split_fc_predict", "ws_split_fc_top1", "ws_combine_top1",

@@ -220,7 +220,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t w4_biases(const W4Args& a) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.bias), 0, a.bias != nullptr ? (int)(4u * (uint32_t)a.C) : 0, 0x00020000);
 }
 __device__ __forceinline__ f32x4 w4_bias(__amdgpu_buffer_rsrc_t biases, int cls) {
-    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, 4 * cls, 0, 0));
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, (int)(4u * (uint32_t)cls), 0, 0));
 }
 
 // Four neighbouring logits, of which the first `n` (any number) are there.
@@ -523,7 +523,7 @@ __global__ __launch_bounds__(W4_STREAM_THREADS) void w4_stream(W4Args a, int til
         w4_load(ring[i][0], aim, l, k);
         k += SPAN;
         const bool last = k >= a.D;
-        int from = 64 * tile;                                                      // no bias is fetched with the other pieces
+        int from = (int)(64u * (uint32_t)tile);                                    // no bias is fetched with the other pieces: beyond any buffer
         if (!last) from = -1024;
         bias[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, 16 * l.g, from, 0));
         if (last) {

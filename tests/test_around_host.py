@@ -30,6 +30,8 @@ def E(ws):
 def test_limits_are_the_headers(ws):
     text = open(os.path.join(ROOT, "include", "whalesplit.h")).read()
     assert int(re.search(r"#define\s+WS_RMS_NORM_MAX_D\s+(\d+)", text).group(1)) == ws.RMS_NORM_MAX_D
+    power, less = re.search(r"#define\s+WS_W4_MAX_CLASSES\s+\(\(1 << (\d+)\) - (\d+)\)", text).groups()
+    assert (1 << int(power)) - int(less) == ws.W4_MAX_CLASSES
 
 
 def test_norm_refusals(ws, E):

@@ -257,3 +257,30 @@ def test_codes_beyond_four_gigabytes(G):
     Z = torch.empty((1, 80), device="cuda")
     ws.split_fc_w4_logits(X, None, W4[C - 80:], s[C - 80:], None, Z)
     assert float(Z[0, 77]) == 64.0 and float(Z.abs().sum()) == 64.0
+
+
+@pytest.mark.parametrize("B", [1, 40])
+def test_as_many_classes_as_there_may_be(G, B):
+    """2^30 - 65 536 classes: 34 GB of codes, 4 GB of biases; rows of 1, codes of 0 but for one class, the bias of another one outside its part."""
+    import torch
+    from paper_2011_09208_amd import binding as ws
+    D, C = 64, ws.W4_MAX_CLASSES
+    W4 = torch.zeros((C, D // 2), device="cuda", dtype=torch.uint8)
+    s = torch.full((C, D // 32), 127, device="cuda", dtype=torch.uint8)
+    bias = torch.zeros(C, device="cuda")
+    X = torch.ones((B, D), device="cuda", dtype=torch.bfloat16)
+    top, cls = torch.empty(B, device="cuda"), torch.empty(B, device="cuda", dtype=torch.int32)
+    work = torch.empty(ws.w4_top1_workspace_bytes(B, C), device="cuda", dtype=torch.uint8)
+    W4[C - 3] = 0x22                                                                     # codes of 1
+    ws.split_fc_w4_top1(X, None, W4, s, bias, 9, top, cls, work)
+    assert bool((top == 64).all()) and bool((cls == C - 3 + 9).all())
+    bias[C - 1], bias[(1 << 29) + 5] = 65, 64.5
+    ws.split_fc_w4_top1(X, None, W4, s, bias, 9, top, cls, work)
+    assert bool((top == 65).all()) and bool((cls == C - 1 + 9).all())
+    bias[C - 1] = 0
+    ws.split_fc_w4_top1(X, None, W4, s, bias, 9, top, cls, work)
+    assert bool((top == 64.5).all()) and bool((cls == (1 << 29) + 5 + 9).all())
+    if B == 1:
+        Z = torch.full((B, C), -1.0, device="cuda")
+        ws.split_fc_w4_logits(X, None, W4, s, bias, Z)
+        assert float(Z[0, C - 3]) == 64 and float(Z[0, (1 << 29) + 5]) == 64.5 and int((Z != 0).sum()) == 2
