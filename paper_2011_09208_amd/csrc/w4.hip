@@ -573,27 +573,28 @@ __global__ __launch_bounds__(W4_STREAM_THREADS) void w4_stream(W4Args a, int til
 // meet in LDS.  One workgroup per group of classes, most of a compute unit's wave slots filled with them: reading alone, W of 100 000 x 2048
 // takes 16.9 us so, 19.9 with a wave for 16 whole rows; 1000 x 4096 2.8 and 6.8.
 //
-// Wave k takes the steps S k .. S k + S - 1 of CT tiles of 16 classes.  Rows go 16 at a time, and P steps of them at a time through LDS, where
-// each wave has a region of its own.
+// Wave k takes the steps S k .. S k + S - 1 of CT tiles of 16 classes.  Rows go 16 NT at a time, and P steps of them at a time through LDS, where
+// each wave has a region of its own.  Up to 32 rows at a time: 32 x 2048 x 12 500 took 11.2 us in two halves, 64 18.5 in four.
 constexpr int W4_FEW_ROWS = 64;
 constexpr int W4_FEW_WAVES = 8, W4_FEW_THREADS = 64 * W4_FEW_WAVES;
-constexpr int w4_few_piece(int S, int CT, bool MX) { return S >= 2 && S <= 4 && (MX || CT * S == 2) ? 2 : 1; }          // P, as many as the registers hold
+constexpr int w4_few_piece(int S, int CT, int NT, bool MX) { return S >= 2 && S <= 4 && (MX || CT * S * NT == 2) ? 2 : 1; }          // P, as many as the registers hold
 constexpr int w4_few_plane(int P, int rows) { return (rows * (64 * P + 16) + 255) & ~255; }
 constexpr int w4_few_region(int P, int CT, int rows) {
     const int features = 4 * w4_few_plane(P, rows), sums = rows * (16 * CT + 4) * 4;
     return features > sums ? features : (sums + 255) & ~255;
 }
 
-template <int S, int CT, bool MX, bool TOP1>
-__global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4Args a) {
-    constexpr int P = w4_few_piece(S, CT, MX), PITCH = 16 * CT + 4, UNITS = MX ? P * 2 : P * 4;        // 16-byte loads of a lane for a piece of 16 rows
+template <int S, int CT, int NT, bool MX, bool TOP1>
+__global__ __launch_bounds__(W4_FEW_THREADS, S * CT * NT < 8 ? 4 : 2) void w4_few(W4Args a) {
+    constexpr int P = w4_few_piece(S, CT, NT, MX), PITCH = 16 * CT + 4, R = 16 * NT;
+    constexpr int UNITS = (MX ? P * 2 : P * 4) * NT;                               // 16-byte loads of a lane for a piece of R rows
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63;
     const W4Lane l(lane, a);
     const int i16 = l.i16, g = l.g;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int step0 = wave * S;
-    const int most = a.B < 16 ? a.B : 16;
+    const int most = a.B < R ? a.B : R;
     const int plane = w4_few_plane(P, most), region = w4_few_region(P, CT, most);
     char* mine = lds + wave * region;
     const int first = blockIdx.x * 16 * CT;                                        // the workgroup's first class
@@ -609,7 +610,7 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4A
     u32x4 xr[UNITS];
     uint32_t xs[MX ? UNITS : 1];
     auto fetch = [&](int n0, int s) {
-        const int rows = a.B - n0 < 16 ? a.B - n0 : 16;
+        const int rows = a.B - n0 < R ? a.B - n0 : R;
 #pragma unroll
         for (int j = 0; j < UNITS; ++j) {
             const int at = lane + 64 * j, r = at / ROW_UNITS, u = at & (ROW_UNITS - 1);
@@ -644,21 +645,25 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4A
     W4Piece<S> codes[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) w4_load(codes[c], W4Tile(a, busy ? first + 16 * c : a.C), l, step0 * W4_STEP);
-    for (int n0 = 0; n0 < a.B; n0 += 16) {
-        const int rows = a.B - n0 < 16 ? a.B - n0 : 16;
-        f32x4 acc[CT];
+    for (int n0 = 0; n0 < a.B; n0 += R) {
+        const int rows = a.B - n0 < R ? a.B - n0 : R;
+        f32x4 acc[CT][NT];
 #pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (busy) {
             uint32_t joined[CT][W4Piece<S>::HELD];
-            const char* x = mine + g * plane + (i16 < rows ? i16 : rows - 1) * (64 * P + 16);
+            const char* x[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x[n] = mine + g * plane + (16 * n + i16 < rows ? 16 * n + i16 : rows - 1) * (64 * P + 16);
 #pragma unroll
             for (int s0 = 0; s0 < S; s0 += P) {
                 stage(rows);
                 if (s0 + P < S) {
                     fetch(n0, s0 + P);
-                } else if (n0 + 16 < a.B) {
-                    fetch(n0 + 16, 0);
+                } else if (n0 + R < a.B) {
+                    fetch(n0 + R, 0);
                 }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");             // LDS serves a wave's accesses in their order
                 if (s0 == 0)
@@ -676,19 +681,27 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4A
                     }
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const bf16x8 xb = *reinterpret_cast<const bf16x8*>(x + 64 * (s - s0) + 16 * q);
+                        bf16x8 xb[NT];
 #pragma unroll
-                        for (int c = 0; c < CT; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w4_values(v[c][q], f[c]), xb, acc[c], 0, 0, 0);
+                        for (int n = 0; n < NT; ++n) xb[n] = *reinterpret_cast<const bf16x8*>(x[n] + 64 * (s - s0) + 16 * q);
+#pragma unroll
+                        for (int c = 0; c < CT; ++c) {
+                            const bf16x8 wa = w4_values(v[c][q], f[c]);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) acc[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, xb[n], acc[c][n], 0, 0, 0);
+                        }
                     }
                 }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
         }
-        if (i16 < rows) {
-            float* to = reinterpret_cast<float*>(mine) + i16 * PITCH + 4 * g;
 #pragma unroll
-            for (int c = 0; c < CT; ++c) *reinterpret_cast<f32x4*>(to + 16 * c) = acc[c];
-        }
+        for (int n = 0; n < NT; ++n)
+            if (16 * n + i16 < rows) {
+                float* to = reinterpret_cast<float*>(mine) + (16 * n + i16) * PITCH + 4 * g;
+#pragma unroll
+                for (int c = 0; c < CT; ++c) *reinterpret_cast<f32x4*>(to + 16 * c) = acc[c][n];
+            }
         wait_counts<NO_VM_WAIT, 0>();
         raw_barrier();                                                             // loads stay in flight
         const char* from = lds + 16 * c4;
@@ -711,7 +724,7 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT < 8 ? 4 : 2) void w4_few(W4A
                 w4_store(a.Z + (int64_t)(n0 + r) * a.ldz + cls, z, a.C - cls);
             }
         }
-        if (n0 + 16 < a.B) {
+        if (n0 + R < a.B) {
             wait_counts<NO_VM_WAIT, 0>();
             raw_barrier();                                                         // the sums have been read
         }
@@ -747,22 +760,28 @@ static inline bool al(const void* p, size_t a) { return (reinterpret_cast<uintpt
 //   rows x features x classes    w4_stream RING 1, 2    w4_few       w4_tiles
 //    1 x 2048 x 100000           24.0  24.9             29           35
 //   16 x 2048 x 100000           27.0  27.2             31           37
-//   32 x 2048 x 100000           31.4  33.9             47           40
+//   32 x 2048 x 100000           31.4  33.9             51           40
 //    1 x  512 x 100000            8.2  10.3             10.7         11.9
-//    1 x 2048 x 12500             8.2   7.6              7.0         14.0
-//   32 x 2048 x 12500            12.2  11.3             11.2         15.1
+//    1 x 2048 x 12500             8.2   7.6              6.6         14.0
+//   16 x 2048 x 12500             9.6                    7.4
+//   32 x 2048 x 12500            12.2  11.3              9.0         15.1
+//   32 x 2048 x 16000            12.6                    9.7
+//   32 x 2048 x 20000            13.2                   15.6
 //    1 x 8192 x 12500            24.5  17.0             28           47
 //    1 x 4096 x 4000             10.3   8.9              5.4
 //    1 x 4096 x 1000             10.1   8.6              4.8         19.1
 //    8 x  512 x 2000              3.2   4.8              3.9
-//   40 x 2048 x 12500                                   14.0         17.1
-//   64 x  512 x 12500                                   10.0          7.8
-//   64 x 2048 x 3000                                    10.1         16.1
-//   64 x 2048 x 12500                                   18.5         18.9
-//   64 x 2048 x 25000                                   25.3         20.5
-//   64 x 2048 x 100000                                  75           47.6
-// A wave of w4_stream takes whole rows of 16 classes: with few of them most waves have nothing to do, and w4_few shares the rows out.  Its second
-// barrier-bound half costs some 3 us, so short rows and many classes stay on w4_stream, or with more rows than it holds on w4_tiles.
+//   40 x 2048 x 12500                                   12.4         17.1
+//   40 x 2048 x 20000                                   21.9         17.7
+//   64 x  512 x 12500                                    7.8          7.8
+//   64 x 2048 x 3000                                     8.1         16.1
+//   64 x 2048 x 16000                                   14.8         19.0
+//   64 x 2048 x 25000                                   25.9         20.4
+//   64 x 8192 x 4000                                    25.7         56.6
+//   64 x 8192 x 12500                                   83           58
+//   64 x 2048 x 100000                                  82           47.5
+// A wave of w4_stream takes whole rows of 16 classes: with few of them most waves have nothing to do, and w4_few shares the rows out, while its
+// workgroups fit the compute units at once.  Short rows stay on w4_stream, or with more rows of the batch than it holds on w4_tiles.
 enum W4Way { W4_STREAM, W4_FEW, W4_TILES };
 struct W4Plan {
     W4Way way;
@@ -784,7 +803,7 @@ static W4Plan w4_plan(int B, int D, int C, bool top1) {
     const int steps = (D + W4_STEP - 1) / W4_STEP;
     const bool fits = B <= 32 && w4_stream_lds(B, D) <= W4_STREAM_LDS;
     const int64_t most = steps <= 32 ? 1024 : 512;                                 // tiles up to which rows are shared out
-    if (B <= W4_FEW_ROWS && steps >= 8 && steps <= 8 * W4_FEW_WAVES && (fits ? tiles <= most : tiles * ((B + 15) / 16) <= 4 * most)) {
+    if (B <= W4_FEW_ROWS && steps >= 8 && steps <= 8 * W4_FEW_WAVES && tiles <= most) {
         p.way = W4_FEW;
         while (W4_FEW_WAVES * p.S < steps) p.S *= 2;
         // as many classes to a workgroup as the registers hold, while there are workgroups for most compute units
@@ -822,21 +841,21 @@ static int w4_parts(const W4Plan& p, int B) {
     return parts;
 }
 
-template <int S, int CT, bool MX, bool TOP1>
+template <int S, int CT, int NT, bool MX, bool TOP1>
 static void launch_w4_few(const W4Args& a, const W4Plan& f, hipStream_t s) {
-    const size_t bytes = (size_t)W4_FEW_WAVES * w4_few_region(w4_few_piece(S, CT, MX), CT, a.B < 16 ? a.B : 16);
-    hipLaunchKernelGGL((w4_few<S, CT, MX, TOP1>), dim3(f.groups), dim3(W4_FEW_THREADS), bytes, s, a);
+    const size_t bytes = (size_t)W4_FEW_WAVES * w4_few_region(w4_few_piece(S, CT, NT, MX), CT, a.B < 16 * NT ? a.B : 16 * NT);
+    hipLaunchKernelGGL((w4_few<S, CT, NT, MX, TOP1>), dim3(f.groups), dim3(W4_FEW_THREADS), bytes, s, a);
 }
 
-template <bool MX, bool TOP1>
+template <int NT, bool MX, bool TOP1>
 static void launch_w4_steps(const W4Args& a, const W4Plan& f, hipStream_t s) {
     switch (f.S * 8 + f.CT) {
-        case 1 * 8 + 4: return launch_w4_few<1, 4, MX, TOP1>(a, f, s);
-        case 2 * 8 + 1: return launch_w4_few<2, 1, MX, TOP1>(a, f, s);
-        case 2 * 8 + 4: return launch_w4_few<2, 4, MX, TOP1>(a, f, s);
-        case 4 * 8 + 1: return launch_w4_few<4, 1, MX, TOP1>(a, f, s);
-        case 4 * 8 + 2: return launch_w4_few<4, 2, MX, TOP1>(a, f, s);
-        default: return launch_w4_few<8, 1, MX, TOP1>(a, f, s);
+        case 1 * 8 + 4: return launch_w4_few<1, 4, NT, MX, TOP1>(a, f, s);
+        case 2 * 8 + 1: return launch_w4_few<2, 1, NT, MX, TOP1>(a, f, s);
+        case 2 * 8 + 4: return launch_w4_few<2, 4, NT, MX, TOP1>(a, f, s);
+        case 4 * 8 + 1: return launch_w4_few<4, 1, NT, MX, TOP1>(a, f, s);
+        case 4 * 8 + 2: return launch_w4_few<4, 2, NT, MX, TOP1>(a, f, s);
+        default: return launch_w4_few<8, 1, NT, MX, TOP1>(a, f, s);
     }
 }
 
@@ -858,7 +877,7 @@ static void launch_w4_stream(const W4Args& a, const W4Plan& p, hipStream_t s) {
 template <bool MX, bool TOP1>
 static void launch_w4_type(const W4Args& a, hipStream_t s) {
     const W4Plan p = w4_plan(a.B, a.D, a.C, TOP1);
-    if (p.way == W4_FEW) return launch_w4_steps<MX, TOP1>(a, p, s);
+    if (p.way == W4_FEW) return a.B > 16 ? launch_w4_steps<2, MX, TOP1>(a, p, s) : launch_w4_steps<1, MX, TOP1>(a, p, s);
     if (p.way == W4_STREAM) {
         if (a.B > 16) return launch_w4_stream<2, 1, MX, TOP1>(a, p, s);
         return p.ring == 1 ? launch_w4_stream<1, 1, MX, TOP1>(a, p, s) : launch_w4_stream<1, 2, MX, TOP1>(a, p, s);
