@@ -568,14 +568,14 @@ __global__ __launch_bounds__(W4_STREAM_THREADS) void w4_stream(W4Args a, int til
     if constexpr (TOP1) w4_report<NT, W4_STREAM_WAVES>(a, best, best_at, 0, rows, l, lds, blockIdx.x, gridDim.x);
 }
 
-// ---- few rows --------------------------------------------------------------------------------------------------------
+// ---- few tiles of rows and classes -----------------------------------------------------------------------------------
 // The waves of a workgroup share out the contraction, so that all codes of its classes are on their way at once, and the waves' partial sums
 // meet in LDS.  One workgroup per group of classes, most of a compute unit's wave slots filled with them: reading alone, W of 100 000 x 2048
 // takes 16.9 us so, 19.9 with a wave for 16 whole rows; 1000 x 4096 2.8 and 6.8.
 //
 // Wave k takes the steps S k .. S k + S - 1 of CT tiles of 16 classes.  Rows go 16 NT at a time, and P steps of them at a time through LDS, where
-// each wave has a region of its own.  Up to 32 rows at a time: 32 x 2048 x 12 500 took 11.2 us in two halves, 64 18.5 in four.
-constexpr int W4_FEW_ROWS = 64;
+// each wave has a region of its own.  Up to 32 rows at a time: 32 x 2048 x 12 500 took 11.2 us in
+// two halves, 64 18.5 in four.  Blocks of rows go side by side where units are free: 128 x 2048 x 3000 14.4 us one after the other, 7.9.
 constexpr int W4_FEW_WAVES = 8, W4_FEW_THREADS = 64 * W4_FEW_WAVES;
 constexpr int w4_few_piece(int S, int CT, int NT, bool MX) { return S >= 2 && S <= 4 && (MX || CT * S * NT == 2) ? 2 : 1; }          // P, as many as the registers hold
 constexpr int w4_few_plane(int P, int rows) { return (rows * (64 * P + 16) + 255) & ~255; }
@@ -594,6 +594,7 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT * NT < 8 ? 4 : 2) void w4_fe
     const int i16 = l.i16, g = l.g;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int step0 = wave * S;
+    const int row0 = blockIdx.y * R, stride = gridDim.y * R;
     const int most = a.B < R ? a.B : R;
     const int plane = w4_few_plane(P, most), region = w4_few_region(P, CT, most);
     char* mine = lds + wave * region;
@@ -641,11 +642,11 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT * NT < 8 ? 4 : 2) void w4_fe
     };
     const int steps = (a.D + W4_STEP - 1) / W4_STEP;
     const bool busy = step0 < steps;                                               // waves beyond the contraction only add up
-    if (busy) fetch(0, 0);                                                         // from the cache, and staged while the codes are on their way
+    if (busy) fetch(row0, 0);                                                         // from the cache, and staged while the codes are on their way
     W4Piece<S> codes[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) w4_load(codes[c], W4Tile(a, busy ? first + 16 * c : a.C), l, step0 * W4_STEP);
-    for (int n0 = 0; n0 < a.B; n0 += R) {
+    for (int n0 = row0; n0 < a.B; n0 += stride) {
         const int rows = a.B - n0 < R ? a.B - n0 : R;
         f32x4 acc[CT][NT];
 #pragma unroll
@@ -662,8 +663,8 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT * NT < 8 ? 4 : 2) void w4_fe
                 stage(rows);
                 if (s0 + P < S) {
                     fetch(n0, s0 + P);
-                } else if (n0 + R < a.B) {
-                    fetch(n0 + R, 0);
+                } else if (n0 + stride < a.B) {
+                    fetch(n0 + stride, 0);
                 }
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");             // LDS serves a wave's accesses in their order
                 if (s0 == 0)
@@ -724,7 +725,7 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT * NT < 8 ? 4 : 2) void w4_fe
                 w4_store(a.Z + (int64_t)(n0 + r) * a.ldz + cls, z, a.C - cls);
             }
         }
-        if (n0 + R < a.B) {
+        if (n0 + stride < a.B) {
             wait_counts<NO_VM_WAIT, 0>();
             raw_barrier();                                                         // the sums have been read
         }
@@ -771,23 +772,29 @@ static inline bool al(const void* p, size_t a) { return (reinterpret_cast<uintpt
 //    1 x 4096 x 4000             10.3   8.9              5.4
 //    1 x 4096 x 1000             10.1   8.6              4.8         19.1
 //    8 x  512 x 2000              3.2   4.8              3.9
-//   40 x 2048 x 12500                                   12.4         17.1
-//   40 x 2048 x 20000                                   21.9         17.7
+//   64 x 1024 x 1000                                     4.9         10.2
 //   64 x  512 x 12500                                    7.8          7.8
-//   64 x 2048 x 3000                                     8.1         16.1
-//   64 x 2048 x 16000                                   14.8         19.0
+//   40 x 2048 x 12500                                   12.2         17.1
+//   64 x 2048 x 12500                                   14.3         18.9
 //   64 x 2048 x 25000                                   25.9         20.4
-//   64 x 8192 x 4000                                    25.7         56.6
-//   64 x 8192 x 12500                                   83           58
-//   64 x 2048 x 100000                                  82           47.5
+//   96 x 2048 x 12500                                   19.7         18.7
+//  128 x 2048 x 3000                                     7.9         16.1
+//  128 x 2048 x 12500                                   24.9         19.8
+//  256 x 2048 x 1000                                     8.5         16.0
+//  256 x 2048 x 8000                                    24.4         19.1
+//  128 x 4096 x 4000                                    15.6         29.0
+//  256 x 4096 x 1000                                     8.7         27.4
+//  128 x 8192 x 1000                                    12.4         50
+//  256 x 8192 x 4000                                    75           56
 // A wave of w4_stream takes whole rows of 16 classes: with few of them most waves have nothing to do, and w4_few shares the rows out, while its
-// workgroups fit the compute units at once.  Short rows stay on w4_stream, or with more rows of the batch than it holds on w4_tiles.
+// workgroups fit the compute units at once.  Short rows stay on w4_stream, or with more rows of the batch than it holds on w4_tiles, whose time per
+// step hardly depends on how many tiles there are: w4_few is faster up to two rounds of its workgroups.
 enum W4Way { W4_STREAM, W4_FEW, W4_TILES };
 struct W4Plan {
     W4Way way;
     int groups;                              // workgroups along the classes
     int ring;                                // w4_stream
-    int S, CT;                               // w4_few
+    int S, CT, row_groups;                   // w4_few
     int NT;                                  // w4_tiles
     bool wide;                               //   eight waves, not four
 };
@@ -798,18 +805,23 @@ static size_t w4_stream_lds(int B, int D) {
     return 4 * (((size_t)B * (64 * steps + 16) + 255) & ~(size_t)255);
 }
 static W4Plan w4_plan(int B, int D, int C, bool top1) {
-    W4Plan p = {W4_TILES, 0, 1, 1, 1, 0, false};
+    W4Plan p = {W4_TILES, 0, 1, 1, 1, 1, 0, false};
     const int64_t tiles = ((int64_t)C + 15) / 16;
     const int steps = (D + W4_STEP - 1) / W4_STEP;
     const bool fits = B <= 32 && w4_stream_lds(B, D) <= W4_STREAM_LDS;
     const int64_t most = steps <= 32 ? 1024 : 512;                                 // tiles up to which rows are shared out
-    if (B <= W4_FEW_ROWS && steps >= 8 && steps <= 8 * W4_FEW_WAVES && tiles <= most) {
+    const int row_blocks = (B + 31) / 32;
+    if (steps >= 8 && steps <= 8 * W4_FEW_WAVES && (fits ? tiles <= most : tiles * row_blocks <= 2 * most)) {
         p.way = W4_FEW;
         while (W4_FEW_WAVES * p.S < steps) p.S *= 2;
-        // as many classes to a workgroup as the registers hold, while there are workgroups for most compute units
+        // as many classes to a workgroup as the registers hold, while there are workgroups for most compute units; with the 32 rows' features in
+        // LDS one workgroup fits a unit, and more of them than units would go one after the other (32 x 4096 x 6000 13.4 us, 9.5)
         p.CT = p.S <= 2 ? 4 : p.S == 4 ? 2 : 1;
-        if (p.S > 1 && tiles < 192 * p.CT) p.CT = 1;
+        if (p.S > 1 && (B <= 16 ? tiles < 192 * p.CT : tiles * row_blocks <= 256)) p.CT = 1;
         p.groups = (int)((tiles + p.CT - 1) / p.CT);
+        // blocks of rows side by side as far as there are compute units, evenly many one after the other
+        const int side = p.groups < 256 ? 256 / p.groups : 1, turns = (row_blocks + side - 1) / side;
+        p.row_groups = (row_blocks + turns - 1) / turns;
     } else if (fits) {
         p.way = W4_STREAM;
         p.groups = tiles < 256 ? (int)tiles : 256;
@@ -844,7 +856,7 @@ static int w4_parts(const W4Plan& p, int B) {
 template <int S, int CT, int NT, bool MX, bool TOP1>
 static void launch_w4_few(const W4Args& a, const W4Plan& f, hipStream_t s) {
     const size_t bytes = (size_t)W4_FEW_WAVES * w4_few_region(w4_few_piece(S, CT, NT, MX), CT, a.B < 16 * NT ? a.B : 16 * NT);
-    hipLaunchKernelGGL((w4_few<S, CT, NT, MX, TOP1>), dim3(f.groups), dim3(W4_FEW_THREADS), bytes, s, a);
+    hipLaunchKernelGGL((w4_few<S, CT, NT, MX, TOP1>), dim3(f.groups, f.row_groups), dim3(W4_FEW_THREADS), bytes, s, a);
 }
 
 template <int NT, bool MX, bool TOP1>

@@ -119,7 +119,8 @@ def test_logits_and_top1(G, B, D, C, x_kind):
 # number of steps), tiles of rows and classes (narrow and wide ones of every height)
 LARGE = [(1, 512, 20000), (9, 2048, 17000), (32, 1984, 17000), (1, 4224, 9000), (3, 1024, 2000), (20, 1088, 3100), (5, 2048, 1000), (64, 2048, 5000),
          (7, 4096, 8000), (31, 4096, 500), (1, 4224, 300), (40, 8192, 2000), (20, 8256, 300), (20, 8256, 42000), (50, 576, 1000), (64, 512, 42001),
-         (40, 1024, 2000), (33, 2048, 12500), (5, 2048, 12400), (31, 4096, 8000), (2, 4096, 300), (17, 1984, 300), (64, 4160, 500), (40, 64, 45000), (96, 576, 83000), (100, 128, 90003), (73, 128, 90003), (128, 320, 83001), (250, 64, 45000)]
+         (40, 1024, 2000), (33, 2048, 12500), (5, 2048, 12400), (31, 4096, 8000), (2, 4096, 300), (17, 1984, 300), (64, 4160, 500), (100, 2048, 3000), (200, 1024, 4000), (129, 8192, 1000),
+         (2000, 1024, 200), (70, 4096, 1500), (40, 64, 45000), (96, 576, 83000), (100, 128, 90003), (73, 128, 90003), (128, 320, 83001), (250, 64, 45000)]
 
 
 def _device_layer(B, D, C, x_kind, seed):
