@@ -289,7 +289,10 @@ __device__ __forceinline__ void w4_report(const W4Args& a, float (&best)[NT], in
 // Up to 64 rows CT = 2 leaves registers for two workgroups on a compute unit, which fill each other's pauses (64 x 256 x 100 000 classes 15.2 us,
 // CT = 4 17.8); with more rows CT = 4 halves what is read from LDS for a product.
 //
-// Tried and slower: the codes of two steps on their way (64 x 2048 x 100 000 classes 48.8 us, now 47.4); the scales of 16 steps through LDS
+// With four waves, where a compute unit has no second workgroup, two steps of codes and features are on their way (96 x 2048 x 12 500 18.7 us, now
+// 17.8; 20 x 10 240 x 3000 61, 47).
+//
+// Tried and slower: the same with eight waves (64 x 2048 x 100 000 classes 48.8 us, now 47.4); the scales of 16 steps through LDS
 // (a step of 64 rows is 15 % faster, but the start costs 7 us: 200 x 1088 x 50 001 49.6 us, otherwise 39.8).
 //
 // Logits leave through LDS, one c after the other, in a loop that is not unrolled: straight from the accumulators every one of the CT NT 4 stores
@@ -302,6 +305,7 @@ __global__ __launch_bounds__(64 * WAVES, CT == 2 && WAVES == 8 ? 4 : 2) void w4_
     constexpr int OUT_BYTES = R * OUT_PITCH * 4;
     constexpr int UNITS = (R * 8 + THREADS - 1) / THREADS;                         // of 16 features that a thread brings to LDS in a step
     constexpr bool EARLY = CT * NT <= 24;                                          // registers for the next step's codes in the product's order, too
+    constexpr int SETS = WAVES == 4 ? 2 : 1;                                       // steps on their way
     __shared__ __attribute__((aligned(16))) char lds[2 * HALF > OUT_BYTES ? 2 * HALF : OUT_BYTES];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const W4Lane l(tid & 63, a);
@@ -341,7 +345,7 @@ __global__ __launch_bounds__(64 * WAVES, CT == 2 && WAVES == 8 ? 4 : 2) void w4_
     struct Rows {
         u32x4 a[UNITS], b[UNITS];
         uint32_t s[UNITS];
-    } coming;
+    } coming[SETS];
     // No branch around the loads; beyond the row's end, half a step at most, the last features are loaded once more and zeros are staged.
     auto fetch = [&](Rows& w, int step) {
         const int s = step < steps ? step : steps - 1;
@@ -375,41 +379,46 @@ __global__ __launch_bounds__(64 * WAVES, CT == 2 && WAVES == 8 ? 4 : 2) void w4_
 
     for (int group = first; group < groups; group += parts) {
         const int class0 = group * CLASSES + wave * 16;
-        W4Piece<1> codes[CT];
-        auto load = [&](int step) {
+        W4Piece<1> codes[SETS][CT];
+        auto load = [&](W4Piece<1> (&p)[CT], int step) {
 #pragma unroll
-            for (int c = 0; c < CT; ++c) w4_load(codes[c], W4Tile(a, class0 + STRIP * c), l, step * W4_STEP);
+            for (int c = 0; c < CT; ++c) w4_load(p[c], W4Tile(a, class0 + STRIP * c), l, step * W4_STEP);
         };
         float f[CT];                                                               // codes and scales in the product's order
         u32x4 v[CT];
-        auto take = [&](float (&to_f)[CT], u32x4 (&to_v)[CT], int c, int step) {
+        auto take = [&](float (&to_f)[CT], u32x4 (&to_v)[CT], const W4Piece<1> (&p)[CT], int c, int step) {
             uint32_t joined[1];
-            w4_join(joined, codes[c]);
+            w4_join(joined, p[c]);
             to_f[c] = w4_scale<false>(joined, 0, a.D - step * W4_STEP, l);
-            to_v[c] = w4_codes(codes[c], 0, l);
+            to_v[c] = w4_codes(p[c], 0, l);
         };
         f32x4 acc[CT][NT];
 #pragma unroll
         for (int c = 0; c < CT; ++c)
 #pragma unroll
             for (int n = 0; n < NT; ++n) acc[c][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        fetch(coming, 0);
-        load(0);
-        stage(coming, 0);
+        fetch(coming[0], 0);
+        load(codes[0], 0);
+        if constexpr (SETS == 2) {
+            fetch(coming[1], 1);
+            load(codes[1], 1);
+        }
+        stage(coming[0], 0);
         if constexpr (EARLY) {
 #pragma unroll
-            for (int c = 0; c < CT; ++c) take(f, v, c, 0);
-            load(1);
+            for (int c = 0; c < CT; ++c) take(f, v, codes[0], c, 0);
+            load(codes[0], SETS);
         }
         wait_counts<NO_VM_WAIT, 0>();
         raw_barrier();
-#pragma unroll 1
-        for (int step = 0; step < steps; ++step) {
-            fetch(coming, step + 1);
+        // `p` holds the codes of this step, or of the next one if they are taken early; `free` and `next` are the rows' features behind the next step
+        // and of it.  Loads return in order: features that came from the cache one step ahead would wait for the codes two steps ahead.
+        auto turn = [&](W4Piece<1> (&p)[CT], Rows& free, const Rows& next, int step) {
+            fetch(free, step + SETS);
             if constexpr (!EARLY) {
 #pragma unroll
-                for (int c = 0; c < CT; ++c) take(f, v, c, step);
-                load(step + 1);
+                for (int c = 0; c < CT; ++c) take(f, v, p, c, step);
+                load(p, step + 1);
             }
             // Fragments of the features are read three ahead, and the codes of the next quarter of a step turned into values meanwhile; the order is
             // pinned, left alone the reads end up right in front of their products and the loads behind them.
@@ -434,7 +443,7 @@ __global__ __launch_bounds__(64 * WAVES, CT == 2 && WAVES == 8 ? 4 : 2) void w4_
                 if (EARLY && q >= 2)                                               // the next step's codes, a tile at a time in the second half of this one
 #pragma unroll
                     for (int c = 0; c < CT; ++c)
-                        if (c == (i - 2 * NT) * CT / (2 * NT) && (i == 2 * NT || c != (i - 1 - 2 * NT) * CT / (2 * NT))) take(next_f, next_v, c, step + 1);
+                        if (c == (i - 2 * NT) * CT / (2 * NT) && (i == 2 * NT || c != (i - 1 - 2 * NT) * CT / (2 * NT))) take(next_f, next_v, p, c, step + 1);
 #pragma unroll
                 for (int c = 0; c < CT; ++c) acc[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[c], ring[i & 3], acc[c][n], 0, 0, 0);
                 if (n == NT - 1)
@@ -443,17 +452,22 @@ __global__ __launch_bounds__(64 * WAVES, CT == 2 && WAVES == 8 ? 4 : 2) void w4_
                 __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (EARLY) {
-                load(step + 2);
+                load(p, step + 1 + SETS);
 #pragma unroll
                 for (int c = 0; c < CT; ++c) {
                     f[c] = next_f[c];
                     v[c] = next_v[c];
                 }
             }
-            stage(coming, step + 1);
+            stage(next, step + 1);
             wait_counts<NO_VM_WAIT, 0>();
             raw_barrier();                                                         // the codes stay in flight
-        }
+        };
+#pragma unroll 1
+        for (int step = 0; step < steps; step += SETS)
+#pragma unroll
+            for (int i = 0; i < SETS; ++i)                                         // a step too many adds zeros
+                turn(codes[EARLY ? (i + 1) % SETS : i], coming[i], coming[(i + 1) % SETS], step + i);
         float* out = reinterpret_cast<float*>(lds);
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
@@ -776,16 +790,16 @@ static inline bool al(const void* p, size_t a) { return (reinterpret_cast<uintpt
 //   64 x  512 x 12500                                    7.8          7.8
 //   40 x 2048 x 12500                                   12.2         17.1
 //   64 x 2048 x 12500                                   14.3         18.9
-//   64 x 2048 x 25000                                   25.9         20.4
-//   96 x 2048 x 12500                                   19.7         18.7
+//   64 x 2048 x 25000                                   25.9         19.0
+//   96 x 2048 x 12500                                   19.7         17.8
 //  128 x 2048 x 3000                                     7.9         16.1
-//  128 x 2048 x 12500                                   24.9         19.8
+//  128 x 2048 x 12500                                   24.9         18.7
 //  256 x 2048 x 1000                                     8.5         16.0
 //  256 x 2048 x 8000                                    24.4         19.1
 //  128 x 4096 x 4000                                    15.6         29.0
 //  256 x 4096 x 1000                                     8.7         27.4
 //  128 x 8192 x 1000                                    12.4         50
-//  256 x 8192 x 4000                                    75           56
+//  256 x 8192 x 4000                                    75           52
 // A wave of w4_stream takes whole rows of 16 classes: with few of them most waves have nothing to do, and w4_few shares the rows out, while its
 // workgroups fit the compute units at once.  Short rows stay on w4_stream, or with more rows of the batch than it holds on w4_tiles, whose time per
 // step hardly depends on how many tiles there are: w4_few is faster up to two rounds of its workgroups.
