@@ -62,14 +62,15 @@ __device__ __forceinline__ void store_stream(void* base, int64_t at, const f32x8
     else *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(base) + at) = pack8(f);
 }
 
-// Sum over the 64 lanes, the same in every lane and in the same order whatever the lane.
-__device__ __forceinline__ float wave_sum(float v) {
+// Sum over groups of T neighbouring lanes, the same in all of them and in the same order whatever the lane.
+template <int T>
+__device__ __forceinline__ float lane_sum(float v) {
     v += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0xB1, 0xF, 0xF, true));     // lane ^ 1
     v += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x4E, 0xF, 0xF, true));     // lane ^ 2
     v += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x141, 0xF, 0xF, true));    // the other quad of eight
-    v += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x140, 0xF, 0xF, true));    // the other half of sixteen
-    v += __shfl_xor(v, 16, 64);
-    v += __shfl_xor(v, 32, 64);
+    if (T >= 16) v += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), 0x140, 0xF, 0xF, true));    // the other half of sixteen
+    if (T >= 32) v += __shfl_xor(v, 16, 64);
+    if (T >= 64) v += __shfl_xor(v, 32, 64);
     return v;
 }
 
@@ -77,7 +78,7 @@ __device__ __forceinline__ float wave_sum(float v) {
 // call's barrier if calls alternate between two of them.
 template <int T>
 __device__ __forceinline__ float row_sum(float v, float* part) {
-    v = wave_sum(v);
+    v = lane_sum<T>(v);
     if constexpr (T > 64) {
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
         __syncthreads();
@@ -88,14 +89,15 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
     return v;
 }
 
-// T threads take a row, NV pieces of eight features each, in steps of 8 T: D <= 8 T NV.  A wave for a row needs no barrier.
+// T threads take a row, NV pieces of eight features each, in steps of 8 T: D <= 8 T NV.  A wave for a row needs no barrier; short rows share one (the
+// rows of a norm over 64 features: 65 536 of them 23.5 us with a wave for each).
 template <int T, int NV, bool FP32, bool MX>
 __global__ __launch_bounds__(T > 256 ? T : 256) void rms_norm_fwd(NormArgs a) {
     constexpr int ROWS = T > 256 ? 1 : 256 / T;
-    __shared__ float part[T / 64];
+    __shared__ float part[T > 64 ? T / 64 : 1];
     const int t = threadIdx.x % T;
     const int row = blockIdx.x * ROWS + threadIdx.x / T;
-    if (T == 64 && row >= a.B) return;                     // T > 64: one row to a workgroup, and as many workgroups as rows
+    if (T <= 64 && row >= a.B) return;                     // T > 64: one row to a workgroup, and as many workgroups as rows
     const int n = a.D >> 3;
     const uint16_t* x = a.x + row * a.ldx;
     f32x8 h[NV];
@@ -180,13 +182,14 @@ struct NormBackArgs {
 // pairs 8.4.
 constexpr int NORM_BACK_WAVES = 8;
 constexpr int norm_back_threads(int T) { return T > 64 ? T : 64 * NORM_BACK_WAVES; }
+constexpr int norm_back_rows(int T) { return T > 64 ? 1 : norm_back_threads(T) / T; }
 
 template <int T, int NV, bool FP32>
 __global__ __launch_bounds__(norm_back_threads(T)) void rms_norm_bwd(NormBackArgs a) {
-    static_assert(T > 64 || 64 * NV * 8 <= 4 * norm_back_threads(T), "a thread for four columns");
-    constexpr int ROWS = T > 64 ? 1 : NORM_BACK_WAVES;
-    __shared__ float part[2][T / 64];
-    __shared__ __attribute__((aligned(16))) float meet[T == 64 ? ROWS * 64 * NV * 8 : 1];
+    constexpr int ROWS = norm_back_rows(T), COLS = 8 * T * NV;
+    static_assert(T > 64 || COLS <= 4 * norm_back_threads(T), "a thread for four columns");
+    __shared__ float part[2][T > 64 ? T / 64 : 1];
+    __shared__ __attribute__((aligned(16))) float meet[T <= 64 ? NORM_BACK_WAVES * COLS : 1];
     const int t = threadIdx.x % T, r = threadIdx.x / T;
     const int n = a.D >> 3;
     f32x8 sum[NV];
@@ -239,16 +242,22 @@ __global__ __launch_bounds__(norm_back_threads(T)) void rms_norm_bwd(NormBackArg
         }
     }
     if (a.parts == nullptr) return;
-    if constexpr (T == 64) {             // the waves' shares, each thread four columns of all of them
-        constexpr int COLS = 64 * NV * 8;
+    if constexpr (T <= 64) {             // rows that share a wave, then the waves' shares, each thread four columns of all of them
 #pragma unroll
-        for (int k = 0; k < NV; ++k) store8(meet + r * COLS + 512 * k + 8 * t, sum[k]);
+        for (int m = T; m < 64; m <<= 1)
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[k][e] += __shfl_xor(sum[k][e], m, 64);
+        if ((threadIdx.x & 63) < T)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) store8(meet + (threadIdx.x >> 6) * COLS + 8 * (T * k + t), sum[k]);
         __syncthreads();
         const int c = 4 * threadIdx.x;
         if (c < a.D) {
             f32x4 v = *reinterpret_cast<const f32x4*>(meet + c);
 #pragma unroll
-            for (int w = 1; w < ROWS; ++w) v += *reinterpret_cast<const f32x4*>(meet + w * COLS + c);
+            for (int w = 1; w < NORM_BACK_WAVES; ++w) v += *reinterpret_cast<const f32x4*>(meet + w * COLS + c);
             *reinterpret_cast<f32x4*>(a.parts + (int64_t)blockIdx.x * a.D + c) = v;
         }
     } else {
@@ -281,7 +290,7 @@ __global__ __launch_bounds__(256) void rms_norm_dgamma(const float* __restrict__
 
 // Workgroups of the backward call: each leaves a share of dgamma that has to be written and read again.
 static int norm_back_groups(int B, int D) {
-    const int rows = D <= 2048 ? NORM_BACK_WAVES : 1, most = D <= 2048 ? 256 : 512;
+    const int rows = norm_back_rows(D <= 64 ? 8 : D <= 128 ? 16 : D <= 256 ? 32 : D <= 2048 ? 64 : 256), most = D <= 2048 ? 256 : 512;
     const int groups = (B + rows - 1) / rows;
     return groups < most ? groups : most;
 }
@@ -309,7 +318,10 @@ template <bool FP32, bool MX>
 static void launch_norm(NormArgs a, hipStream_t s) {
     for (int left = a.B; left > 0; left -= NORM_SLICE) {
         a.B = left < NORM_SLICE ? left : NORM_SLICE;
-        if (a.D <= 512) hipLaunchKernelGGL((rms_norm_fwd<64, 1, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
+        if (a.D <= 64) hipLaunchKernelGGL((rms_norm_fwd<8, 1, FP32, MX>), dim3((a.B + 31) / 32), dim3(256), 0, s, a);
+        else if (a.D <= 128) hipLaunchKernelGGL((rms_norm_fwd<16, 1, FP32, MX>), dim3((a.B + 15) / 16), dim3(256), 0, s, a);
+        else if (a.D <= 256) hipLaunchKernelGGL((rms_norm_fwd<32, 1, FP32, MX>), dim3((a.B + 7) / 8), dim3(256), 0, s, a);
+        else if (a.D <= 512) hipLaunchKernelGGL((rms_norm_fwd<64, 1, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
         else if (a.D <= 1024) hipLaunchKernelGGL((rms_norm_fwd<64, 2, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
         else if (a.D <= 2048) hipLaunchKernelGGL((rms_norm_fwd<64, 4, FP32, MX>), dim3((a.B + 3) / 4), dim3(256), 0, s, a);
         else if (a.D <= 4096) hipLaunchKernelGGL((rms_norm_fwd<256, 2, FP32, MX>), dim3(a.B), dim3(256), 0, s, a);
@@ -326,7 +338,10 @@ static void launch_norm(NormArgs a, hipStream_t s) {
 
 template <bool FP32>
 static void launch_norm_back(const NormBackArgs& a, int groups, hipStream_t s) {
-    if (a.D <= 512) hipLaunchKernelGGL((rms_norm_bwd<64, 1, FP32>), dim3(groups), dim3(norm_back_threads(64)), 0, s, a);
+    if (a.D <= 64) hipLaunchKernelGGL((rms_norm_bwd<8, 1, FP32>), dim3(groups), dim3(norm_back_threads(8)), 0, s, a);
+    else if (a.D <= 128) hipLaunchKernelGGL((rms_norm_bwd<16, 1, FP32>), dim3(groups), dim3(norm_back_threads(16)), 0, s, a);
+    else if (a.D <= 256) hipLaunchKernelGGL((rms_norm_bwd<32, 1, FP32>), dim3(groups), dim3(norm_back_threads(32)), 0, s, a);
+    else if (a.D <= 512) hipLaunchKernelGGL((rms_norm_bwd<64, 1, FP32>), dim3(groups), dim3(norm_back_threads(64)), 0, s, a);
     else if (a.D <= 1024) hipLaunchKernelGGL((rms_norm_bwd<64, 2, FP32>), dim3(groups), dim3(norm_back_threads(64)), 0, s, a);
     else if (a.D <= 2048) hipLaunchKernelGGL((rms_norm_bwd<64, 4, FP32>), dim3(groups), dim3(norm_back_threads(64)), 0, s, a);
     else if (a.D <= 4096) hipLaunchKernelGGL((rms_norm_bwd<256, 2, FP32>), dim3(groups), dim3(256), 0, s, a);

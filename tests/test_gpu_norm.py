@@ -7,8 +7,9 @@ from tests import mx_formats as mx
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24                                            # half a step of fp32, relative
 HALF = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}            # of the types that results are rounded to
-# D: one piece per lane and a quarter of a wave, each number of pieces, a ragged last piece, a workgroup for a row, a large one, the largest
-SIZES = [(1, 64), (3, 64), (5, 512), (2, 576), (7, 1024), (9, 1088), (4, 2048), (1, 2112), (3, 4096), (2, 4160), (3, 8192), (2, 8256), (2, 16384), (531, 320)]
+# D: one piece per lane and an eighth to a whole wave, each number of pieces, a ragged last piece, a workgroup for a row, a large one, the largest
+SIZES = [(1, 64), (3, 64), (5, 512), (2, 576), (7, 1024), (9, 1088), (4, 2048), (1, 2112), (3, 4096), (2, 4160), (3, 8192), (2, 8256), (2, 16384), (531, 320),
+         (5, 128), (37, 192), (19, 256), (1000, 256)]
 
 
 @pytest.fixture(scope="module")
