@@ -7,6 +7,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/whalesplit.h"
 #include "mx.h"
 
@@ -198,31 +200,53 @@ __global__ __launch_bounds__(norm_back_threads(T)) void rms_norm_bwd(NormBackArg
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[k][e] = 0.0f;
     int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + r; row < a.B; row += (int64_t)gridDim.x * ROWS) {
-        f32x8 gy[NV], xh[NV];
-        const float rstd = a.rstd[row];
-        float dot = 0.0f;
+    // the next row is on its way while this one is finished (4096 x 2048 bf16 20.4 us without, 18.2; 2048 x 8192 40.7, 34.1)
+    f32x8 dy[NV];
+    typedef typename std::conditional<FP32, f32x8, u32x4>::type Raw;
+    Raw hv[NV];
+    float next_rstd;
+    auto load_raw = [&](const void* base, int64_t at, Raw& v) {
+        if constexpr (FP32) load8(static_cast<const float*>(base) + at, v);
+        else v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + at);
+    };
+    auto fetch = [&](int64_t row) {
+        next_rstd = a.rstd[row];
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = t + k * T;
             if (c >= n) continue;
-            load8(a.dY + row * a.lddy + 8 * c, gy[k]);
-            load_stream<FP32>(a.h, row * a.ldh + 8 * c, xh[k]);
+            load8(a.dY + row * a.lddy + 8 * c, dy[k]);
+            load_raw(a.h, row * a.ldh + 8 * c, hv[k]);
         }
+    };
+    const int64_t first = (int64_t)blockIdx.x * ROWS + r, stride = (int64_t)gridDim.x * ROWS;
+    if (first < a.B) fetch(first);
+    for (int64_t row = first; row < a.B; row += stride) {
+        f32x8 gy[NV], xh[NV];
+        const float rstd = next_rstd;
+        float dot = 0.0f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = t + k * T;
             if (c >= n) continue;
             f32x8 g;
             load8(a.gamma + 8 * c, g);
+            if constexpr (!FP32) unpack8(hv[k], xh[k]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
+                if constexpr (FP32) xh[k][e] = hv[k][e];
                 xh[k][e] *= rstd;
-                sum[k][e] = fmaf(gy[k][e], xh[k][e], sum[k][e]);
-                gy[k][e] *= g[e];
+                sum[k][e] = fmaf(dy[k][e], xh[k][e], sum[k][e]);
+                gy[k][e] = dy[k][e] * g[e];
                 dot = fmaf(gy[k][e], xh[k][e], dot);
             }
         }
+        Raw through[NV];                                       // before the next row's loads: they return in order
+        if (a.dres != nullptr)
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (t + k * T < n) load_raw(a.dres, row * a.ldd + 8 * (t + k * T), through[k]);
+        if (row + stride < a.B) fetch(row + stride);
         dot = row_sum<T>(dot, part[turn]) / (float)a.D;
         turn ^= 1;
 #pragma unroll
@@ -233,10 +257,13 @@ __global__ __launch_bounds__(norm_back_threads(T)) void rms_norm_bwd(NormBackArg
 #pragma unroll
             for (int e = 0; e < 8; ++e) d[e] = rstd * fmaf(-dot, xh[k][e], gy[k][e]);
             if (a.dres != nullptr) {
-                f32x8 through;
-                load_stream<FP32>(a.dres, row * a.ldd + 8 * c, through);
+                f32x8 more;
+                if constexpr (!FP32) unpack8(through[k], more);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] += through[e];
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (FP32) more[e] = through[k][e];
+                    d[e] += more[e];
+                }
             }
             store_stream<FP32>(a.dh, row * a.lddh + 8 * c, d);
         }
