@@ -313,7 +313,7 @@ struct TensorList {
 
 // Chunks of a tensor as the kernels count them, for_each_chunk.
 static int64_t chunks_of(const void* data, int64_t rows, int64_t cols, int32_t bytes) {
-    if (rows == 1) return (cols + (int64_t)(reinterpret_cast<uintptr_t>(data) & 15) / bytes + GRAD_CHUNK - 1) / GRAD_CHUNK;
+    if (rows == 1) return (cols + (int64_t)((reinterpret_cast<uintptr_t>(data) & 15) >> (bytes == 4 ? 2 : 1)) + GRAD_CHUNK - 1) / GRAD_CHUNK;
     if (cols > GRAD_CHUNK / 2) return rows * ((cols + GRAD_CHUNK - 1) / GRAD_CHUNK);
     return (rows + GRAD_CHUNK / cols - 1) / (GRAD_CHUNK / cols);
 }
@@ -330,7 +330,7 @@ static int check_tensors(const TensorList& l, int32_t n) {
         // chunks are counted in 30 bits
         if (l.cols[i] > (int64_t)1 << 42 || (l.rows[i] > 1 && l.cols[i] > ((int64_t)1 << 42) / l.rows[i])) return WS_ERR_RANGE;
         if (l.rows[i] > 1 && chunks_of(l.data[i], l.rows[i], l.cols[i], l.bytes[i]) > INT32_MAX / 2) return WS_ERR_RANGE;
-        if (reinterpret_cast<uintptr_t>(l.data[i]) % (uintptr_t)l.bytes[i]) return WS_ERR_ALIGN;
+        if (reinterpret_cast<uintptr_t>(l.data[i]) & (uintptr_t)(l.bytes[i] - 1)) return WS_ERR_ALIGN;
     }
     return WS_OK;
 }
