@@ -777,32 +777,33 @@ static inline bool al(const void* p, size_t a) { return (reinterpret_cast<uintpt
 //   16 x 2048 x 100000           27.0  27.2             31           37
 //   32 x 2048 x 100000           31.4  33.9             51           40
 //    1 x  512 x 100000            8.2  10.3             10.7         11.9
-//    1 x 2048 x 12500             8.2   7.6              6.6         14.0
-//   16 x 2048 x 12500             9.6                    7.4
-//   32 x 2048 x 12500            12.2  11.3              9.0         15.1
-//   32 x 2048 x 16000            12.6                    9.7
-//   32 x 2048 x 20000            13.2                   15.6
-//    1 x 8192 x 12500            24.5  17.0             28           47
-//    1 x 4096 x 4000             10.3   8.9              5.4
-//    1 x 4096 x 1000             10.1   8.6              4.8         19.1
-//    8 x  512 x 2000              3.2   4.8              3.9
-//   64 x 1024 x 1000                                     4.9         10.2
-//   64 x  512 x 12500                                    7.8          7.8
-//   40 x 2048 x 12500                                   12.2         17.1
-//   64 x 2048 x 12500                                   14.3         18.9
-//   64 x 2048 x 25000                                   25.9         19.0
+//    1 x 2048 x 12500             8.2   7.6              6.6         11.6
+//   16 x 2048 x 12500             9.6                    7.4         12.3
+//   32 x 2048 x 12500            12.2  11.3              9.0         13.0
+//   32 x 2048 x 16000            12.6                    9.7         13.2
+//   32 x 2048 x 20000            13.2                   15.6         13.4
+//    1 x 8192 x 12500            24.5  17.0             28           37
+//    1 x 4096 x 4000             10.3   8.9              5.4         17.8
+//    1 x 4096 x 1000             10.1   8.6              4.8         17.4
+//    8 x  512 x 2000              3.2   4.8              3.9          4.7
+//   64 x  512 x 12500                                    7.8          6.3
+//   64 x 1024 x 1000                                     4.9          7.7
+//   64 x 1024 x 12500                                    8.4          8.7
+//   40 x 2048 x 12500                                   12.2         12.5
+//   64 x 2048 x 12500                                   14.3         13.4
 //   96 x 2048 x 12500                                   19.7         17.8
-//  128 x 2048 x 3000                                     7.9         16.1
-//  128 x 2048 x 12500                                   24.9         18.7
-//  256 x 2048 x 1000                                     8.5         16.0
-//  256 x 2048 x 8000                                    24.4         19.1
-//  128 x 4096 x 4000                                    15.6         29.0
-//  256 x 4096 x 1000                                     8.7         27.4
-//  128 x 8192 x 1000                                    12.4         50
-//  256 x 8192 x 4000                                    75           52
+//  128 x 2048 x 3000                                     7.9         11.7
+//  256 x 2048 x 3000                                    12.3         11.9
+//   64 x 4096 x 6000                                    15.2         21.3
+//   96 x 4096 x 6000                                    21.4         21.6
+//  128 x 4096 x 6000                                    27.3         21.5
+//   64 x 4096 x 12500                                   29.3         22.0
+//  256 x 4096 x 1000                                     8.7         19.2
+//  128 x 8192 x 1000                                    12.4         34
+//  256 x 8192 x 4000                                    75           36
 // A wave of w4_stream takes whole rows of 16 classes: with few of them most waves have nothing to do, and w4_few shares the rows out, while its
 // workgroups fit the compute units at once.  Short rows stay on w4_stream, or with more rows of the batch than it holds on w4_tiles, whose time per
-// step hardly depends on how many tiles there are: w4_few is faster up to two rounds of its workgroups.
+// step hardly depends on how many tiles there are: w4_few is faster for less than two rounds of its workgroups.
 enum W4Way { W4_STREAM, W4_FEW, W4_TILES };
 struct W4Plan {
     W4Way way;
@@ -823,9 +824,9 @@ static W4Plan w4_plan(int B, int D, int C, bool top1) {
     const int64_t tiles = ((int64_t)C + 15) / 16;
     const int steps = (D + W4_STEP - 1) / W4_STEP;
     const bool fits = B <= 32 && w4_stream_lds(B, D) <= W4_STREAM_LDS;
-    const int64_t most = steps <= 32 ? 1024 : 512;                                 // tiles up to which rows are shared out
     const int row_blocks = (B + 31) / 32;
-    if (steps >= 8 && steps <= 8 * W4_FEW_WAVES && (fits ? tiles <= most : tiles * row_blocks <= 2 * most)) {
+    const int64_t most = fits ? (steps <= 32 ? 1024 : 512) : steps <= 8 ? 2048 : steps <= 16 ? 1536 : 1024;      // 16 classes x 32 rows shared out
+    if (steps >= 8 && steps <= 8 * W4_FEW_WAVES && tiles * row_blocks <= most) {
         p.way = W4_FEW;
         while (W4_FEW_WAVES * p.S < steps) p.S *= 2;
         // as many classes to a workgroup as the registers hold, while there are workgroups for most compute units; with the 32 rows' features in
@@ -844,15 +845,16 @@ static W4Plan w4_plan(int B, int D, int C, bool top1) {
         const int row_tiles = (B + 15) / 16;
         // Blocks of rows of one height, up to 8 tiles of 16 with CT = 4 tiles of classes, up to 4 with CT = 2; eight waves to a workgroup, or four.  The
         // tall ones for logits only (the arg-max's candidates take registers, too: 256 x 2048 x 100 000 153 us with 6 tiles, 134 with 4), and
-        // whatever is larger only while there are workgroups for most compute units (80 x 2048 x 50 000: 45 us with four waves, 42 with eight).
+        // whatever is larger only while there are workgroups for most compute units (80 x 2048 x 50 000: 45 us with four waves, 42 with eight);
+        // two tiles of 16 rows if that makes a workgroup for each at most (64 x 4096 x 12 500 29.3 us with four, 22.0; 128 of these rows 30.4, 33.5).
         auto shape = [&](int most_rows, int classes) {
             const int blocks = (row_tiles + most_rows - 1) / most_rows;
             p.NT = (row_tiles + blocks - 1) / blocks;
             p.groups = (int)((tiles + classes - 1) / classes);
-            return (int64_t)p.groups * blocks >= 160;
+            return (int64_t)p.groups * blocks;
         };
-        p.wide = (!top1 && row_tiles > 4 && shape(8, 32)) || shape(4, 16);
-        if (!p.wide) shape(4, 8);
+        p.wide = (!top1 && row_tiles > 4 && shape(8, 32) >= 160) || shape(4, 16) >= 160;
+        if (!p.wide && shape(2, 8) > 256) shape(4, 8);
         if (p.NT <= 4) p.NT = p.NT <= 2 ? 2 : 4;
     }
     return p;
