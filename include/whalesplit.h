@@ -309,6 +309,8 @@ int ws_rms_norm_bwd(const float* dY, int64_t lddy, const void* h, int64_t ldh, c
  *                          16-byte aligned, pitch a multiple of 4; columns beyond C_shard are not touched
  *   ws_split_fc_w4_top1    the arg-max of the same logits, which are not written: outputs, ties and merging over shards as
  *                          for ws_split_fc_top1 and ws_combine_top1; workspace of ws_w4_top1_workspace_bytes
+ * Both calls add the products of a logit in the same order for the same B, D and C_shard; for other sizes the order, and with it
+ * the rounding of the fp32 sums, may differ.
  * X_scales NULL: X is bf16 [B][ldx], ldx in elements.  Else X is e4m3 [B][ldx] with scales [B][ldxs].  Weights and features are
  * multiplied as the values they stand for, with fp32 sums; a product of value and scale beyond bf16's range is not supported.
  * No matrix is limited to 4 GiB here; at most WS_W4_MAX_ROWS rows to a call and WS_W4_MAX_PITCH bytes to a pitch of codes or

@@ -164,6 +164,8 @@ def test_every_division_of_the_work(G, B, D, C, x_kind):
     assert bool(((at >= 0) & (at < C)).all())
     assert bool(((top.vec().double()[:, None] - want.gather(1, at)).abs() <= slack.gather(1, at)).all())
     assert bool((want.gather(1, at)[:, 0] >= want.max(1).values - 2 * slack.max(1).values).all())
+    # both calls add the products of a logit in one order
+    assert torch.equal(top.vec(), Z.t.max(1).values) and torch.equal(Z.t.gather(1, at)[:, 0], top.vec())
 
 
 def test_as_many_rows_as_there_may_be(G):
