@@ -193,7 +193,10 @@ int ws_split_fc_predict(const void* X, int64_t ldx, const void* W_shard, int64_t
  *   ws_split_fc_top1   top_logit[i] = max_c z[i][c],  top_class[i] = class_offset + argmax_c z[i][c]
  *                      (fp32 / int32 [B]); workspace of ws_fwd_workspace_bytes
  *   ws_combine_top1    top_logit / top_class [S][shard_stride] -> best_logit / best_class [B]
- * The comparison is made on the fp32 logits the kernel computes. */
+ * The comparison is made on the fp32 logits the kernel computes.  A NaN logit never wins.  A row of ws_split_fc_top1 without a logit
+ * above -infinity reports -infinity and the class INT32_MAX, which is no class; ws_combine_top1 takes any other shard's candidate
+ * before it.  A row without a candidate that compares gets the NaN candidate of the lowest class (ws_split_fc_w4_top1 reports such),
+ * and without one -infinity and INT32_MAX. */
 int ws_split_fc_top1(const void* X, int64_t ldx, const void* W_shard, int64_t ldw, const float* b_shard,
                      int32_t B, int32_t D, int32_t C_shard, int32_t class_offset,
                      float* top_logit, int32_t* top_class,
@@ -308,7 +311,9 @@ int ws_rms_norm_bwd(const float* dY, int64_t lddy, const void* h, int64_t ldh, c
  *   ws_split_fc_w4_logits  Z[i][c] = sum_d X[i][d] * W[c][d] + b_shard[c]    fp32 [B][ldz], as ws_sp2_reduce_stats reads it:
  *                          16-byte aligned, pitch a multiple of 4; columns beyond C_shard are not touched
  *   ws_split_fc_w4_top1    the arg-max of the same logits, which are not written: outputs, ties and merging over shards as
- *                          for ws_split_fc_top1 and ws_combine_top1; workspace of ws_w4_top1_workspace_bytes
+ *                          for ws_split_fc_top1 and ws_combine_top1; workspace of ws_w4_top1_workspace_bytes.  A class is
+ *                          always one of the shard's: the lowest of a row of -infinity, and a row of nothing but NaN
+ *                          (as features with a scale byte 255 make it) reports NaN and class_offset
  * Both calls add the products of a logit in the same order for the same B, D and C_shard; for other sizes the order, and with it
  * the rounding of the fp32 sums, may differ.
  * X_scales NULL: X is bf16 [B][ldx], ldx in elements.  Else X is e4m3 [B][ldx] with scales [B][ldxs].  Weights and features are

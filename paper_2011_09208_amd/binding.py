@@ -470,7 +470,8 @@ def w4_top1_workspace_bytes(B, C_shard):
 
 
 def split_fc_w4_top1(X, X_scales, W4, W_scales, b_shard, class_offset, top_logit, top_class, workspace):
-    """top_logit fp32 [B], top_class int32 [B] <- the shard's best class per row; inputs as split_fc_w4_logits."""
+    """top_logit fp32 [B], top_class int32 [B] <- the shard's best class per row (NaN and class_offset for a row of NaN); inputs as
+    split_fc_w4_logits."""
     dev = _here(X)
     a = _w4_args(X, X_scales, W4, W_scales, b_shard, dev)
     _check(lib.ws_split_fc_w4_top1(*a, int(class_offset), _vector(top_logit, a[9], _FP32, dev), _vector(top_class, a[9], _I32, dev),

@@ -746,7 +746,8 @@ __global__ __launch_bounds__(W4_FEW_THREADS, S * CT * NT < 8 ? 4 : 2) void w4_fe
     }
 }
 
-// The arg-max's candidates of a row, `parts` of them, shard-local classes, one workgroup to a row.
+// The arg-max's candidates of a row, `parts` of them, shard-local classes, one workgroup to a row.  Any logit that compares, -infinity too, leaves a
+// candidate with a class; a row without one has nothing but NaNs, and reports that with the shard's first class.
 __global__ __launch_bounds__(256) void w4_merge_top1(const float* __restrict__ val, const int* __restrict__ cls, int parts, int class_offset,
                                                      float* __restrict__ top_logit, int* __restrict__ top_class) {
     __shared__ float sv[4];
@@ -764,8 +765,9 @@ __global__ __launch_bounds__(256) void w4_merge_top1(const float* __restrict__ v
     if (threadIdx.x == 0) {
 #pragma unroll
         for (int w = 1; w < 4; ++w) better_of(best, at, sv[w], sc[w]);
-        top_logit[blockIdx.x] = best;
-        top_class[blockIdx.x] = at == INT_MAX ? at : at + class_offset;
+        const bool compares = at != INT_MAX;
+        top_logit[blockIdx.x] = compares ? best : __uint_as_float(0x7fc00000u);
+        top_class[blockIdx.x] = compares ? at + class_offset : class_offset;
     }
 }
 

@@ -1147,10 +1147,21 @@ __global__ __launch_bounds__(NTHREADS) void top1_logits(FcArgs a, float* __restr
     }
 }
 
-// Merges n candidates per row, `stride` apart; `base` is added to the winning class.  One workgroup takes 16 rows:
+// A row none of whose n candidates compares: the NaN among them that has the lowest class, if there is one.
+__device__ __forceinline__ void first_nan(float& v, int& c, const float* val, const int* cls, int n, int64_t stride, int i) {
+    for (int t = 0; t < n; ++t)
+        if (val[t * stride + i] != val[t * stride + i] && cls[t * stride + i] < c) {
+            v = val[t * stride + i];
+            c = cls[t * stride + i];
+        }
+}
+
+// Merges n candidates per row, `stride` apart; `base` is added to the winning class.  NANS: candidates may be NaN (the partial results of
+// ws_split_fc_top1 never are).  One workgroup takes 16 rows:
 // thread (r, q) folds candidates q, q + 64, ... of row r, then the 64 winners of a row are merged through LDS (the better
 // of two is an order, so the grouping does not matter).  With one thread per row the loads of a row followed each
 // other: 391 candidates took 129 us, now 5 us.
+template <bool NANS>
 __global__ __launch_bounds__(1024) void merge_top1(const float* __restrict__ val, const int* __restrict__ cls, int n,
                                                    int64_t stride, int B, int base, float* __restrict__ out_val,
                                                    int* __restrict__ out_cls) {
@@ -1186,6 +1197,7 @@ __global__ __launch_bounds__(1024) void merge_top1(const float* __restrict__ val
         __syncthreads();
     }
     if (q == 0 && i < B) {
+        if (NANS && c == INT_MAX) first_nan(v, c, val, cls, n, stride, i);
         out_val[i] = v;
         out_cls[i] = c == INT_MAX ? c : c + base;
     }
@@ -1195,6 +1207,7 @@ __global__ __launch_bounds__(1024) void merge_top1(const float* __restrict__ val
 // than it saves.  B = 1024, us, here and above: 1 candidate 1.9 and 2.8, 8: 2.2 and 2.7, 12: 2.7 and 2.8, 16: 2.9 and 2.8, 64: 7.4
 // and 3.2 (B = 8192: 12: 2.8 and 3.3, 64: 7.4 and 4.1).
 constexpr int MERGE_FEW = 12;
+template <bool NANS>
 __global__ __launch_bounds__(64) void merge_top1_few(const float* __restrict__ val, const int* __restrict__ cls, int n,
                                                      int64_t stride, int B, int base, float* __restrict__ out_val,
                                                      int* __restrict__ out_cls) {
@@ -1215,6 +1228,7 @@ __global__ __launch_bounds__(64) void merge_top1_few(const float* __restrict__ v
         for (int k = 0; k < MERGE_BATCH; ++k)
             if (t0 + k < n) better_of(v, c, tv[k], tc[k]);
     }
+    if (NANS && c == INT_MAX) first_nan(v, c, val, cls, n, stride, i);
     out_val[i] = v;
     out_cls[i] = c == INT_MAX ? c : c + base;
 }
@@ -2322,12 +2336,17 @@ int ws_split_fc_bwd_sgd(const void* X, int64_t ldx, void* W_shard, int64_t ldw, 
                    dX_partial, lddx, accumulate_dx, W_shard, ldw, b_shard, workspace, workspace_bytes, stream, 1, lr);
 }
 
-static void launch_merge_top1(const float* val, const int* cls, int n, int64_t stride, int B, int base, float* out_val,
+static void launch_merge_top1(const float* val, const int* cls, int n, int64_t stride, int B, int base, bool nans, float* out_val,
                               int* out_cls, hipStream_t s) {
-    if (n <= MERGE_FEW)
-        WS_LAUNCH(KID_TOP1_MERGE, merge_top1_few, dim3((B + 63) / 64), dim3(64), s, val, cls, n, stride, B, base, out_val, out_cls);
-    else
-        WS_LAUNCH(KID_TOP1_MERGE, merge_top1, dim3((B + 15) / 16), dim3(1024), s, val, cls, n, stride, B, base, out_val, out_cls);
+    if (n <= MERGE_FEW) {
+        const dim3 grid((B + 63) / 64), block(64);
+        if (nans) WS_LAUNCH(KID_TOP1_MERGE, merge_top1_few<true>, grid, block, s, val, cls, n, stride, B, base, out_val, out_cls);
+        else WS_LAUNCH(KID_TOP1_MERGE, merge_top1_few<false>, grid, block, s, val, cls, n, stride, B, base, out_val, out_cls);
+    } else {
+        const dim3 grid((B + 15) / 16), block(1024);
+        if (nans) WS_LAUNCH(KID_TOP1_MERGE, merge_top1<true>, grid, block, s, val, cls, n, stride, B, base, out_val, out_cls);
+        else WS_LAUNCH(KID_TOP1_MERGE, merge_top1<false>, grid, block, s, val, cls, n, stride, B, base, out_val, out_cls);
+    }
 }
 
 int ws_split_fc_predict(const void* X, int64_t ldx, const void* W_shard, int64_t ldw, const float* b_shard,
@@ -2400,7 +2419,7 @@ int ws_split_fc_top1(const void* X, int64_t ldx, const void* W_shard, int64_t ld
     } else {
         WS_LAUNCH(KID_TOP1, top1_logits, dim3(xcd_grid(a.nBT * a.nCT)), dim3(NTHREADS), s, a, part_val, part_cls);
     }
-    launch_merge_top1(part_val, part_cls, parts, pitch, B, class_offset, top_logit, top_class, s);
+    launch_merge_top1(part_val, part_cls, parts, pitch, B, class_offset, false, top_logit, top_class, s);
     return launch_status();
 }
 
@@ -2412,7 +2431,7 @@ int ws_combine_top1(const float* top_logit, const int32_t* top_class, int32_t S,
     if (!aligned(top_logit, 4) || !aligned(top_class, 4) || !aligned(best_logit, 4) || !aligned(best_class, 4))
         return WS_ERR_ALIGN;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    launch_merge_top1(top_logit, top_class, S, shard_stride, B, 0, best_logit, best_class, s);
+    launch_merge_top1(top_logit, top_class, S, shard_stride, B, 0, true, best_logit, best_class, s);
     return launch_status();
 }
 
