@@ -58,7 +58,7 @@ struct W4Args {
 
 constexpr int W4_MAX_ROWS = WS_W4_MAX_ROWS;
 constexpr int64_t W4_MAX_PITCH = WS_W4_MAX_PITCH;                            // 16 rows are addressed with 31 bits
-constexpr int W4_MAX_CLASSES = WS_W4_MAX_CLASSES;                            // a whole last group's biases are addressed with 32 bits
+constexpr int W4_MAX_CLASSES = WS_W4_MAX_CLASSES;                            // a whole last group's biases are addressed with 32 bits, the last KiB of them left over
 constexpr int W4_STEP = 128;                 // features that the lanes of a wave cover with 16 bytes of codes each
 
 // Where a lane loads and where its data goes.  A load takes 16 bytes of codes a lane, four neighbouring lanes 64 bytes of a class row: 16 rows x 64
@@ -77,7 +77,10 @@ struct W4Lane {
 };
 
 // Sixteen class rows of codes and of scales as buffers: what lies beyond the last class reads as zeros, without a branch.  A branch around
-// loads, even one that is never taken, makes the compiler wait for them as if nothing had been loaded since.
+// loads, even one that is never taken, makes the compiler wait for them as if nothing had been loaded since.  A step's first byte is the loads'
+// scalar offset: a load is in range if lane offset + scalar offset lies within the buffer, as a sum that does not wrap (measured, make_operand), so the
+// steps behind the last class's last feature read nothing.  (The first byte in the lanes' offsets spills registers in w4_tiles, and so does a buffer for
+// each step.)
 struct W4Tile {
     __amdgpu_buffer_rsrc_t codes, scales;
     // classes [cls, cls + 16) of the shard; none of them if cls >= C
@@ -537,9 +540,9 @@ __global__ __launch_bounds__(W4_STREAM_THREADS) void w4_stream(W4Args a, int til
         w4_load(ring[i][0], aim, l, k);
         k += SPAN;
         const bool last = k >= a.D;
-        int from = (int)(64u * (uint32_t)tile);                                    // no bias is fetched with the other pieces: beyond any buffer
-        if (!last) from = -1024;
-        bias[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, 16 * l.g, from, 0));
+        uint32_t from = 64u * (uint32_t)tile;                                      // no bias is fetched with the other pieces: beyond any buffer
+        if (!last) from = 0u - 1024u;
+        bias[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(biases, (int)(from + 16u * (uint32_t)l.g), 0, 0));
         if (last) {
             k = 0;
             tile = tile + stride < tiles ? tile + stride : tiles;
