@@ -5,9 +5,9 @@ and takes torch tensors that already live on the GPU; torch is used for device
 memory and the current stream, nothing else.  There is no CPU fallback: if the
 library has not been built, importing this module raises.
 """
-import array
 import ctypes
 import os
+import struct
 from operator import attrgetter
 
 import torch
@@ -478,47 +478,64 @@ def split_fc_w4_top1(X, X_scales, W4, W_scales, b_shard, class_offset, top_logit
                                    *_scratch(workspace, dev), _stream()))
 
 
-_ONES = array.array("q", [1]) * 4096
+_ONES = struct.pack("q", 1) * 4096
+_ELEM_BYTES = {kind: struct.pack("i", n) for kind, n in _STREAM_TYPES.items()}
+
+
+def _int64s(values):
+    return struct.pack("%dq" % len(values), *values)
 
 
 class grad_table:
     """The tables that grad_sumsq, grad_clip and grad_clip_sgd take, of bf16 or fp32 device tensors that are contiguous, or
-    matrices with contiguous rows.  It holds addresses: build it again when tensors move."""
+    matrices with contiguous rows.  It holds addresses: build it again when tensors move or change their shapes."""
 
     def __init__(self, tensors, by_rows=False):
         self.tensors = tensors = list(tensors)
         self.n = n = len(tensors)
         T = torch.Tensor
-        kinds = list(map(attrgetter("dtype"), tensors))
-        if len(set(kinds)) == 1:
-            elem_bytes = array.array("i", [_STREAM_TYPES[kinds[0]]]) * n
-        else:
-            elem_bytes = array.array("i", list(map(_STREAM_TYPES.__getitem__, kinds)))
+        self.bytes = b"".join(map(_ELEM_BYTES.__getitem__, map(attrgetter("dtype"), tensors)))
         places = set(map(T.get_device, tensors))
         self.device = _here(tensors[0]) if tensors else None
         assert len(places) <= 1
-        if not by_rows and n <= len(_ONES) and all(map(T.is_contiguous, tensors)):       # each one long row
-            rows = _ONES
-            lds = cols = array.array("q", list(map(T.numel, tensors)))
-        else:
-            rows, cols, lds = [array.array("q") for _ in range(3)]
-            for t in tensors:
-                if t.dim() == 2:
-                    (r, c), (ld, unit) = t.shape, t.stride()
-                    assert unit == 1 or c <= 1
-                else:
-                    assert t.is_contiguous()
-                    r, c, ld = 1, t.numel(), 0
-                rows.append(r)
-                cols.append(c)
-                lds.append(ld if r > 1 else c)
-        data = array.array("q", list(map(T.data_ptr, tensors)))
-        self._arrays = (data, rows, cols, lds, elem_bytes)                   # they own what the addresses point at
-        self.data, self.rows, self.cols, self.lds, self.bytes = [a.buffer_info()[0] for a in self._arrays]
+        self.flat = n == 0 or not by_rows and 8 * n <= len(_ONES) and all(map(T.is_contiguous, tensors))       # each one long row
+        self.data = _int64s(list(map(T.data_ptr, tensors)))
+        self._shapes = None
+        self._extents = None if self.flat else tuple(map(_int64s, zip(*map(self._by_rows, tensors))))
 
+    # What a call does not need is not asked of 100 tensors (the clipped update takes its extents from the gradients); a table that is kept asks once.
     @property
     def extents(self):
-        return self._arrays[1][:self.n], self._arrays[2]
+        """Rows, columns and pitches."""
+        if self._extents is None:
+            cols = _int64s(list(map(torch.Tensor.numel, self.tensors)))
+            self._extents = _ONES, cols, cols
+        return self._extents
+
+    @property
+    def shapes(self):
+        if self._shapes is None:
+            self._shapes = list(map(attrgetter("shape"), self.tensors))
+        return self._shapes
+
+    @staticmethod
+    def _by_rows(t):
+        """(rows, columns, pitch)"""
+        shape, strides = t.shape, t.stride()
+        while len(shape) > 2 and shape[0] == 1:
+            shape, strides = shape[1:], strides[1:]
+        if len(shape) != 2:
+            assert t.is_contiguous()
+            return 1, t.numel(), t.numel()
+        (r, c), (ld, unit) = shape, strides
+        assert unit == 1 or c <= 1
+        return r, c, ld if r > 1 else c
+
+
+def _without_leading_ones(shape):
+    while len(shape) > 0 and shape[0] == 1:
+        shape = shape[1:]
+    return shape
 
 
 def _table(tensors, dev):
@@ -535,25 +552,29 @@ def grad_sumsq(grads, sumsq, workspace):
     """sumsq fp64 [1] <- the sum of the squares of all gradients (tensors, or their grad_table)."""
     dev = _here(sumsq)
     g = _table(grads, dev)
-    _check(lib.ws_grad_sumsq(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, 1, _F64, dev), *_scratch(workspace, dev), _stream()))
+    _check(lib.ws_grad_sumsq(g.data, *g.extents, g.bytes, g.n, _vector(sumsq, 1, _F64, dev), *_scratch(workspace, dev), _stream()))
 
 
 def grad_clip(grads, sumsq, max_norm, norm=None):
     """Scales the gradients in place by min(1, max_norm / norm), norm = sqrt(sum of sumsq fp64 [S]); norm fp32 [1] or None."""
     S, dev = sumsq.numel(), _here(sumsq)
     g = _table(grads, dev)
-    _check(lib.ws_grad_clip(g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, _F64, dev), S, float(max_norm),
+    _check(lib.ws_grad_clip(g.data, *g.extents, g.bytes, g.n, _vector(sumsq, S, _F64, dev), S, float(max_norm),
                             _vector(norm, 1, torch.float32, dev), _stream()))
 
 
 def grad_clip_sgd(params, grads, sumsq, max_norm, lr, norm=None):
-    """params[i] <- params[i] - lr * k * grads[i] with grad_clip's factor k; the gradients are left as they are."""
+    """params[i] <- params[i] - lr * k * grads[i] with grad_clip's factor k; the gradients are left as they are.  A gradient has its
+    parameter's shape (leading dimensions of 1 aside)."""
     S, dev = sumsq.numel(), _here(sumsq)
     p, g = _table(params, dev), _table(grads, dev)
-    if p.extents != g.extents:                             # one of a pair has a pitch: both are described by their rows
-        p, g = grad_table(p.tensors, True), grad_table(g.tensors, True)
-        assert p.extents == g.extents
-    _check(lib.ws_grad_clip_sgd(p.data, p.lds, p.bytes, g.data, g.rows, g.cols, g.lds, g.bytes, g.n, _vector(sumsq, S, _F64, dev), S,
+    if p.shapes != g.shapes:
+        assert list(map(_without_leading_ones, p.shapes)) == list(map(_without_leading_ones, g.shapes))
+    if not (p.flat and g.flat):                            # one of a pair has a pitch: all are described by their rows
+        p, g = [t if not t.flat else grad_table(t.tensors, True) for t in (p, g)]
+        assert p.extents[:2] == g.extents[:2]
+    ld_params = g.extents[2] if p.flat else p.extents[2]
+    _check(lib.ws_grad_clip_sgd(p.data, ld_params, p.bytes, g.data, *g.extents, g.bytes, g.n, _vector(sumsq, S, _F64, dev), S,
                                 float(max_norm), float(lr), _vector(norm, 1, torch.float32, dev), _stream()))
 
 
