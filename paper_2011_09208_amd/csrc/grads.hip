@@ -199,30 +199,43 @@ __global__ __launch_bounds__(1024) void grad_sumsq_total(const double* __restric
     if (threadIdx.x == 0) *sumsq = sum;
 }
 
-// k of the clipping rule, 0 for a norm that is not finite; the first workgroup also reports the norm.
-__device__ __forceinline__ float clip_factor(const double* sumsq, int S, float max_norm, float* norm) {
-    double total = 0.0;
-    for (int s = 0; s < S; ++s) total += sumsq[s];
-    const double n = sqrt(total);
-    if (norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
-    if (!(n <= 1.7976931348623157e308)) return 0.0f;
-    return n > (double)max_norm ? (float)((double)max_norm / n) : 1.0f;
-}
+// k of the clipping rule, 0 for a norm that is not finite; the first workgroup also reports the norm.  k g is at most max_norm, an ordinary number, where k
+// itself may be far below fp32's range: such a factor is applied in 64 bits.
+struct ClipFactor {
+    double k;
+    float k32;
+    bool tiny;
+    __device__ __forceinline__ ClipFactor(const double* sumsq, int S, float max_norm, float* norm) {
+        double total = 0.0;
+        for (int s = 0; s < S; ++s) total += sumsq[s];
+        const double n = sqrt(total);
+        if (norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
+        k = !(n <= 1.7976931348623157e308) ? 0.0 : n > (double)max_norm ? (double)max_norm / n : 1.0;
+        k32 = (float)k;
+        tiny = k < 1.1754943508222875e-38;                   // 2^-126
+    }
+    // v <- k v; a factor of 0 leaves no NaN behind
+    __device__ __forceinline__ void apply(f32x8& v) const {
+        if (tiny) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = k == 0.0 ? 0.0f : (float)(k * (double)v[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= k32;
+        }
+    }
+};
 
 // The tensors are taken backwards: what the sum of squares has read last may still be in the Infinity Cache.
 __global__ __launch_bounds__(GRAD_THREADS) void grad_clip(GradTable table, const double* __restrict__ sumsq, int S, float max_norm,
                                                           float* __restrict__ norm) {
-    const float k = clip_factor(sumsq, S, max_norm, norm);
-    if (k == 1.0f) return;
+    const ClipFactor factor(sumsq, S, max_norm, norm);
+    if (factor.k32 == 1.0f) return;
     for_each_chunk<true>(table, [&](int t, int row0, int rows, int64_t from, int64_t to) {
         const int64_t ld = table.t[t].ld;
         const bool wide = table.t[t].end2 & 1;
         char* first = table.t[t].data + (row0 * ld + from) * (wide ? 4 : 2);
         const int len = (int)(to - from);
-        auto scaled = [&](f32x8& v) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = k == 0.0f ? 0.0f : k * v[e];              // a factor of 0 leaves no NaN behind
-        };
         auto scale = [&](auto type) {
             typedef decltype(type) T;
             T* g = reinterpret_cast<T*>(first);
@@ -233,7 +246,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_clip(GradTable table, const
                 for (int i = 0; i < GRAD_PIECES; ++i) read8(mine, 8 * GRAD_THREADS * i, GRAD_CHUNK, true, v[i]);
 #pragma unroll
                 for (int i = 0; i < GRAD_PIECES; ++i) {
-                    scaled(v[i]);
+                    factor.apply(v[i]);
                     write8(mine, 8 * GRAD_THREADS * i, GRAD_CHUNK, true, v[i]);
                 }
                 return;
@@ -241,7 +254,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_clip(GradTable table, const
             for_each_piece(g, ld, rows, len, [&](int row, int at) {
                 f32x8 v;
                 read8(g + row * ld, at, len, true, v);
-                scaled(v);
+                factor.apply(v);
                 write8(g + row * ld, at, len, true, v);
             });
         };
@@ -252,8 +265,8 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_clip(GradTable table, const
 
 __global__ __launch_bounds__(GRAD_THREADS) void grad_clip_sgd(UpdateTable table, const double* __restrict__ sumsq, int S, float max_norm, float lr,
                                                               float* __restrict__ norm) {
-    const float k = clip_factor(sumsq, S, max_norm, norm);
-    if (k == 0.0f) return;                                   // a step without a finite norm changes nothing
+    const ClipFactor factor(sumsq, S, max_norm, norm);
+    if (factor.k == 0.0) return;                             // a step without a finite norm changes nothing
     for_each_chunk<true>(table, [&](int t, int row0, int rows, int64_t from, int64_t to) {
         const int64_t ldg = table.t[t].ld, ldp = table.p[t].ld2 >> 1;
         const bool wide_g = table.t[t].end2 & 1, wide_p = table.p[t].ld2 & 1;
@@ -265,9 +278,10 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_clip_sgd(UpdateTable table,
             typedef decltype(p_type) P;
             const G* g = reinterpret_cast<const G*>(g0);
             P* p = reinterpret_cast<P*>(p0);
-            auto updated = [&](f32x8& w, const f32x8& v) {
+            auto updated = [&](f32x8& w, f32x8& v) {
+                factor.apply(v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = fmaf(-lr, k * v[e], w[e]);
+                for (int e = 0; e < 8; ++e) w[e] = fmaf(-lr, v[e], w[e]);
             };
             if (len == GRAD_CHUNK && ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(p)) & 15) == 0) {       // then there is one row
                 const G* mine = g + 8 * threadIdx.x;
