@@ -13,7 +13,7 @@ W4_SRC = os.path.join(PKG, "csrc", "w4.hip")
 GRADS_SRC = os.path.join(PKG, "csrc", "grads.hip")
 HOST_SRC = os.path.join(PKG, "csrc", "balance.cpp")
 SRCS = [SRC, BRIDGE_SRC, SP2_SRC, PROBE_SRC, NORM_SRC, W4_SRC, GRADS_SRC, HOST_SRC]
-DEPS = SRCS + [os.path.join(PKG, "csrc", "mx.h"), os.path.join(PKG, "csrc", "gemm_core.h"), os.path.join(PKG, "csrc", "gemm_stream.h"),
+DEPS = SRCS + [os.path.join(PKG, "csrc", "mx.h"), os.path.join(PKG, "csrc", "w4_plan.h"), os.path.join(PKG, "csrc", "gemm_core.h"), os.path.join(PKG, "csrc", "gemm_stream.h"),
         os.path.join(PKG, "csrc", "gemm_small.h"), os.path.join(PKG, "csrc", "gemm_block.h"),
         os.path.join(PKG, "csrc", "gemm_tiles.h"), os.path.join(PKG, "csrc", "plan.h"),
         os.path.join(os.path.dirname(PKG), "include", "whalesplit.h")]

@@ -14,6 +14,7 @@
 
 #include "../../include/whalesplit.h"
 #include "mx.h"
+#include "w4_plan.h"
 
 namespace ws {
 
@@ -55,11 +56,6 @@ struct W4Args {
     float* Z; int64_t ldz;
     float* part_val; int* part_cls;          // [B][workgroups along the classes]
 };
-
-constexpr int W4_MAX_ROWS = WS_W4_MAX_ROWS;
-constexpr int64_t W4_MAX_PITCH = WS_W4_MAX_PITCH;                            // 16 rows are addressed with 31 bits
-constexpr int W4_MAX_CLASSES = WS_W4_MAX_CLASSES;                            // a whole last group's biases are addressed with 32 bits, the last KiB of them left over
-constexpr int W4_STEP = 128;                 // features that the lanes of a wave cover with 16 bytes of codes each
 
 // Where a lane loads and where its data goes.  A load takes 16 bytes of codes a lane, four neighbouring lanes 64 bytes of a class row: 16 rows x 64
 // bytes, one step of 16 classes.  With a lane for each row, as the matrix instruction has them, every lane is in a cache line of its own and
@@ -593,7 +589,7 @@ __global__ __launch_bounds__(W4_STREAM_THREADS) void w4_stream(W4Args a, int til
 // Wave k takes the steps S k .. S k + S - 1 of CT tiles of 16 classes.  Rows go 16 NT at a time, and P steps of them at a time through LDS, where
 // each wave has a region of its own.  Up to 32 rows at a time: 32 x 2048 x 12 500 took 11.2 us in
 // two halves, 64 18.5 in four.  Blocks of rows go side by side where units are free: 128 x 2048 x 3000 14.4 us one after the other, 7.9.
-constexpr int W4_FEW_WAVES = 8, W4_FEW_THREADS = 64 * W4_FEW_WAVES;
+constexpr int W4_FEW_THREADS = 64 * W4_FEW_WAVES;
 constexpr int w4_few_piece(int S, int CT, int NT, bool MX) { return S >= 2 && S <= 4 && (MX || CT * S * NT == 2) ? 2 : 1; }          // P, as many as the registers hold
 constexpr int w4_few_plane(int P, int rows) { return (rows * (64 * P + 16) + 255) & ~255; }
 constexpr int w4_few_region(int P, int CT, int rows) {
@@ -776,104 +772,6 @@ __global__ __launch_bounds__(256) void w4_merge_top1(const float* __restrict__ v
 
 static inline bool al(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-// How a call is run.  us of the launch, fp32 logits of bf16 features, codes not in any cache (one MI355X):
-//   rows x features x classes    w4_stream RING 1, 2    w4_few       w4_tiles
-//    1 x 2048 x 100000           24.0  24.9             29           35
-//   16 x 2048 x 100000           27.0  27.2             31           37
-//   32 x 2048 x 100000           31.4  33.9             51           40
-//    1 x  512 x 100000            8.2  10.3             10.7         11.9
-//    1 x 2048 x 12500             8.2   7.6              6.6         11.6
-//   16 x 2048 x 12500             9.6                    7.4         12.3
-//   32 x 2048 x 12500            12.2  11.3              9.0         13.0
-//   32 x 2048 x 16000            12.6                    9.7         13.2
-//   32 x 2048 x 20000            13.2                   15.6         13.4
-//    1 x 8192 x 12500            24.5  17.0             28           37
-//    1 x 4096 x 4000             10.3   8.9              5.4         17.8
-//    1 x 4096 x 1000             10.1   8.6              4.8         17.4
-//    8 x  512 x 2000              3.2   4.8              3.9          4.7
-//   64 x  512 x 12500                                    7.8          6.3
-//   64 x 1024 x 1000                                     4.9          7.7
-//   64 x 1024 x 12500                                    8.4          8.7
-//   40 x 2048 x 12500                                   12.2         12.5
-//   64 x 2048 x 12500                                   14.3         13.4
-//   96 x 2048 x 12500                                   19.7         17.8
-//  128 x 2048 x 3000                                     7.9         11.7
-//  256 x 2048 x 3000                                    12.3         11.9
-//   64 x 4096 x 6000                                    15.2         21.3
-//   96 x 4096 x 6000                                    21.4         21.6
-//  128 x 4096 x 6000                                    27.3         21.5
-//   64 x 4096 x 12500                                   29.3         22.0
-//  256 x 4096 x 1000                                     8.7         19.2
-//  128 x 8192 x 1000                                    12.4         34
-//  256 x 8192 x 4000                                    75           36
-// A wave of w4_stream takes whole rows of 16 classes: with few of them most waves have nothing to do, and w4_few shares the rows out, while its
-// workgroups fit the compute units at once.  Short rows stay on w4_stream, or with more rows of the batch than it holds on w4_tiles, whose time per
-// step hardly depends on how many tiles there are: w4_few is faster for less than two rounds of its workgroups.
-enum W4Way { W4_STREAM, W4_FEW, W4_TILES };
-struct W4Plan {
-    W4Way way;
-    int groups;                              // workgroups along the classes
-    int ring;                                // w4_stream
-    int S, CT, row_groups;                   // w4_few
-    int NT;                                  // w4_tiles
-    bool wide;                               //   eight waves, not four
-};
-constexpr int W4_MAX_PARTS = 4096;           // candidates of a row at most
-constexpr size_t W4_STREAM_LDS = 160 * 1024;
-static size_t w4_stream_lds(int B, int D) {
-    const size_t steps = (D + W4_STEP - 1) / W4_STEP;
-    return 4 * (((size_t)B * (64 * steps + 16) + 255) & ~(size_t)255);
-}
-static W4Plan w4_plan(int B, int D, int C, bool top1) {
-    W4Plan p = {W4_TILES, 0, 1, 1, 1, 1, 0, false};
-    const int64_t tiles = ((int64_t)C + 15) / 16;
-    const int steps = (D + W4_STEP - 1) / W4_STEP;
-    const bool fits = B <= 32 && w4_stream_lds(B, D) <= W4_STREAM_LDS;
-    const int row_blocks = (B + 31) / 32;
-    const int64_t most = fits ? (steps <= 32 ? 1024 : 512) : steps <= 8 ? 2048 : steps <= 16 ? 1536 : 1024;      // 16 classes x 32 rows shared out
-    if (steps >= 8 && steps <= 8 * W4_FEW_WAVES && tiles * row_blocks <= most) {
-        p.way = W4_FEW;
-        while (W4_FEW_WAVES * p.S < steps) p.S *= 2;
-        // as many classes to a workgroup as the registers hold, while there are workgroups for most compute units; with the 32 rows' features in
-        // LDS one workgroup fits a unit, and more of them than units would go one after the other (32 x 4096 x 6000 13.4 us, 9.5)
-        p.CT = p.S <= 2 ? 4 : p.S == 4 ? 2 : 1;
-        if (p.S > 1 && (B <= 16 ? tiles < 192 * p.CT : tiles * row_blocks <= 256)) p.CT = 1;
-        p.groups = (int)((tiles + p.CT - 1) / p.CT);
-        // blocks of rows side by side as far as there are compute units, evenly many one after the other
-        const int side = p.groups < 256 ? 256 / p.groups : 1, turns = (row_blocks + side - 1) / side;
-        p.row_groups = (row_blocks + turns - 1) / turns;
-    } else if (fits) {
-        p.way = W4_STREAM;
-        p.groups = tiles < 256 ? (int)tiles : 256;
-        p.ring = steps > 32 && tiles <= 1024 ? 2 : 1;
-    } else {
-        const int row_tiles = (B + 15) / 16;
-        // Blocks of rows of one height, up to 8 tiles of 16 with CT = 4 tiles of classes, up to 4 with CT = 2; eight waves to a workgroup, or four.  The
-        // tall ones for logits only (the arg-max's candidates take registers, too: 256 x 2048 x 100 000 153 us with 6 tiles, 134 with 4), and
-        // whatever is larger only while there are workgroups for most compute units (80 x 2048 x 50 000: 45 us with four waves, 42 with eight);
-        // two tiles of 16 rows if that makes a workgroup for each at most (64 x 4096 x 12 500 29.3 us with four, 22.0; 128 of these rows 30.4, 33.5).
-        auto shape = [&](int most_rows, int classes) {
-            const int blocks = (row_tiles + most_rows - 1) / most_rows;
-            p.NT = (row_tiles + blocks - 1) / blocks;
-            p.groups = (int)((tiles + classes - 1) / classes);
-            return (int64_t)p.groups * blocks;
-        };
-        p.wide = (!top1 && row_tiles > 4 && shape(8, 32) >= 160) || shape(4, 16) >= 160;
-        if (!p.wide && shape(2, 8) > 256) shape(4, 8);
-        if (p.NT <= 4) p.NT = p.NT <= 2 ? 2 : 4;
-    }
-    return p;
-}
-
-// Candidates of a row: one of each workgroup along the classes.  w4_tiles' workgroups walk the groups, and with very many rows there are fewer
-// of them: a launch counts its threads with 32 bits.
-static int w4_parts(const W4Plan& p, int B) {
-    int parts = p.groups < W4_MAX_PARTS ? p.groups : W4_MAX_PARTS;
-    if (p.way == W4_TILES)
-        while ((int64_t)parts * ((B + 31) / 32) > 1 << 20) parts /= 2;
-    return parts;
-}
-
 template <int S, int CT, int NT, bool MX, bool TOP1>
 static void launch_w4_few(const W4Args& a, const W4Plan& f, hipStream_t s) {
     const size_t bytes = (size_t)W4_FEW_WAVES * w4_few_region(w4_few_piece(S, CT, NT, MX), CT, a.B < 16 * NT ? a.B : 16 * NT);
@@ -991,11 +889,10 @@ int ws_split_fc_w4_logits(const void* X, int64_t ldx, const void* X_scales, int6
     return hipGetLastError() == hipSuccess ? WS_OK : WS_ERR_HIP;
 }
 
-// Whatever the number of features: no kernel has more than a candidate for 16 classes, nor more than W4_MAX_PARTS of them.
+// Whatever the number of features.
 size_t ws_w4_top1_workspace_bytes(int32_t B, int32_t C_shard) {
     if (B <= 0 || C_shard <= 0 || B > W4_MAX_ROWS) return 0;
-    const int64_t tiles = ((int64_t)C_shard + 15) / 16;
-    return (size_t)(tiles < W4_MAX_PARTS ? tiles : W4_MAX_PARTS) * B * 8;
+    return (size_t)w4_most_parts(B, C_shard) * B * 8;
 }
 
 int ws_split_fc_w4_top1(const void* X, int64_t ldx, const void* X_scales, int64_t ldxs, const void* W4, int64_t ldw4, const void* W_scales,
