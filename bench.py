@@ -363,7 +363,7 @@ def measure_extras(args, result, ws, torch, dev, X, W, y, B, D, C, work, lse, lo
     # layer's gradients and the clipped update.  lr = 0 keeps W as it is.
     if args.workload == "headline":
         gamma, rstd, dY, dgamma = torch.ones(D, device=dev), torch.empty(B, device=dev), torch.randn((B, D), device=dev), torch.empty(D, device=dev)
-        h, Xn, dh = torch.empty_like(X), torch.empty_like(X), torch.empty_like(X)
+        res, h, Xn, dh = torch.randn_like(X), torch.empty_like(X), torch.empty_like(X), torch.empty_like(X)
         W4, Ws = (torch.empty((C, n), device=dev, dtype=torch.uint8) for n in (D // 2, D // 32))
         dW, Z = torch.randn((C, D), device=dev).to(torch.bfloat16), torch.empty((32, C), device=dev)
         top, cls, sumsq, norm = torch.empty(1, device=dev), torch.empty(1, device=dev, dtype=torch.int32), torch.empty(1, device=dev, dtype=torch.float64), torch.empty(1, device=dev)
@@ -377,7 +377,7 @@ def measure_extras(args, result, ws, torch, dev, X, W, y, B, D, C, work, lse, lo
         packed = C * (D / 2 + D / 32)
         around = {}
         for name, n_bytes, fn in (
-                ("rms_norm_fwd", 8.0 * B * D, lambda: ws.rms_norm_fwd(X, X, gamma, 1e-6, h, Xn, rstd)),
+                ("rms_norm_fwd", 8.0 * B * D, lambda: ws.rms_norm_fwd(X, res, gamma, 1e-6, h, Xn, rstd)),
                 ("rms_norm_bwd", 8.0 * B * D, lambda: ws.rms_norm_bwd(dY, h, None, gamma, rstd, dh, dgamma, aux)),
                 ("quantize_mx4", 2.0 * C * D + packed, lambda: ws.quantize_mx4(W, W4, Ws)),
                 ("split_fc_w4_top1, 1 token", packed, lambda: ws.split_fc_w4_top1(X[:1], None, W4, Ws, None, 0, top, cls, aux)),
