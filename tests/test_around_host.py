@@ -164,3 +164,7 @@ def test_formats_of_the_oracle():
     scales = np.arange(100, 116, dtype=np.uint8).reshape(16, 1)
     c, s = mx.quantize4(mx.values4(codes, scales))
     assert np.array_equal(c, codes) and np.array_equal(s, scales)
+
+
+def test_a_library_with_these_entry_points_has_a_version_of_its_own(ws):
+    assert ws.version() >= 1221                            # 1220 was without them
