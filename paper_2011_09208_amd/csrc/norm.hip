@@ -180,8 +180,9 @@ struct NormBackArgs {
 
 // A workgroup walks rows blockIdx.x * ROWS + .., gridDim.x * ROWS apart, and keeps its share of dgamma in registers: a thread's
 // columns are the same in every row.  Where a wave takes a row, eight waves add theirs up: every share costs a write and a read of D floats
-// (1024 x 2048 with four waves: 11.0 us).  All eight shares meet in LDS at once and the threads share out the columns: 7.4 us, in pairs and pairs of
-// pairs 8.4.
+// (1024 x 2048, this kernel alone, with four waves: 11.0 us).  All eight shares meet in LDS at once and the threads share out the columns: 7.4 us, in
+// pairs and pairs of pairs 8.4; with the next row's loads ahead 6.3.  The sum of the 128 shares, in 64 workgroups, makes that 10.4 (8.2 where the
+// operands are in the Infinity Cache): neither launch has a workgroup for each of the 256 compute units.
 constexpr int NORM_BACK_WAVES = 8;
 constexpr int norm_back_threads(int T) { return T > 64 ? T : 64 * NORM_BACK_WAVES; }
 constexpr int norm_back_rows(int T) { return T > 64 ? 1 : norm_back_threads(T) / T; }

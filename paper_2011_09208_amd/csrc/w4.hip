@@ -1,7 +1,7 @@
 // The split layer with 4-bit weights, for serving: logits and arg-max of a batch of tokens, and the packing of the weights.
 //   z[i][c] = sum_d X[i][d] * W[c][d] + b[c],  W[c][d] = e2m1 code * 2^(scale byte of (c, d / 32) - 127)
-// A batch of tokens reads every weight once and does two flops per token with it, so what bounds it is reading W: half a byte and
-// 1/64 of the scale's byte per weight instead of bf16's two.
+// A batch of tokens reads every weight once and does two flops per token with it, so what bounds it is reading W: half a byte
+// of code and 1/32 of a byte of scale per weight instead of bf16's two.
 //
 // The products run on the bf16 matrix instructions.  A code times its power of two is exact in bf16, and so is an e4m3 feature times
 // its own, so only the fp32 sums round.  (The matrix instructions for 8- and 4-bit operands align the products of a group to the largest and
@@ -284,7 +284,8 @@ __device__ __forceinline__ void w4_report(const W4Args& a, float (&best)[NT], in
 // A wave takes CT x 16 classes and 16 NT rows, a workgroup WAVES waves along the classes; tile c of all waves makes WAVES x 16 neighbouring classes.
 // A step of the rows' features is in LDS, the next one on its way to the other half, and so are the next codes.  A step takes 2.2 us with 64
 // rows, most of it the way of its codes: load, exchange between lanes, conversion, product; with 256 rows the matrix instructions and LDS, from which
-// every wave reads every feature fragment, for CT products each.  200 x 1088 x 50 001: 38.2 us, 128 x 2048 x 100 000: 65 (800 TFLOP/s), 256: 117 (900).
+// every wave reads every feature fragment, for CT products each.  201 x 1088 x 50 001: 38.5 us with
+// codes and logits in HBM, 33.3 where the 69 MB that a call moves are in the Infinity Cache; 128 x 2048 x 100 000: 65 (800 TFLOP/s), 256: 123 (850).
 // Up to 64 rows CT = 2 leaves registers for two workgroups on a compute unit, which fill each other's pauses (64 x 256 x 100 000 classes 15.2 us,
 // CT = 4 17.8); with more rows CT = 4 halves what is read from LDS for a product.
 //
@@ -292,7 +293,7 @@ __device__ __forceinline__ void w4_report(const W4Args& a, float (&best)[NT], in
 // 17.8; 20 x 10 240 x 3000 61, 47).
 //
 // Tried and slower: the same with eight waves (64 x 2048 x 100 000 classes 48.8 us, now 47.4); the scales of 16 steps through LDS
-// (a step of 64 rows is 15 % faster, but the start costs 7 us: 200 x 1088 x 50 001 49.6 us, otherwise 39.8).
+// (a step of 64 rows is 15 % faster, but the start costs 7 us: 200 x 1088 x 50 001 49.6 us, 39.8 for the kernel of then without them).
 //
 // Logits leave through LDS, one c after the other, in a loop that is not unrolled: straight from the accumulators every one of the CT NT 4 stores
 // and bounds checks is code of its own, 10 KiB that each launch fetches anew (128 rows x 256 features x 100 000 classes 28.6 us).

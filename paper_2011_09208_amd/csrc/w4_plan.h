@@ -19,7 +19,7 @@ constexpr int W4_MAX_PARTS = 4096;           // candidates of a row at most
 constexpr int W4_STREAM_GROUPS = 256;        // workgroups of w4_stream at most, one to a compute unit
 constexpr size_t W4_STREAM_LDS = 160 * 1024;
 
-// How a call is run.  us of the launch, fp32 logits of bf16 features, codes not in any cache (one MI355X):
+// How a call is run.  us of the launch, fp32 logits of bf16 features, codes not in any cache (one MI355X); - where a kernel cannot run:
 //   rows x features x classes    w4_stream RING 1, 2    w4_few       w4_tiles
 //    1 x 2048 x 100000           24.0  24.9             29           35
 //   16 x 2048 x 100000           27.0  27.2             31           37
@@ -49,9 +49,22 @@ constexpr size_t W4_STREAM_LDS = 160 * 1024;
 //  256 x 4096 x 1000                                     8.7         19.2
 //  128 x 8192 x 1000                                    12.4         34
 //  256 x 8192 x 4000                                    75           36
+//   19 x 4096 x 100000          50.6                    97           82
+//   20 x 4096 x 100000           -                      94           82
+//   32 x 4096 x 100000           -                     102           84
+//   19 x 4096 x 12500           19.1                    16.5         21.4
+//   20 x 4096 x 12500            -                      16.7         21.5
+//    9 x 8192 x 12500           20.7 (RING 2)           31           38
+//   10 x 8192 x 12500            -                      31           38
+//   32 x 8192 x 12500            -                      45           39
+//    9 x 8192 x 100000         102                                  160
+//   10 x 8192 x 100000           -                                  160
 // A wave of w4_stream takes whole rows of 16 classes: with few of them most waves have nothing to do, and w4_few shares the rows out, while its
 // workgroups fit the compute units at once.  Short rows stay on w4_stream, or with more rows of the batch than it holds on w4_tiles, whose time per
-// step hardly depends on how many tiles there are: w4_few is faster for less than two rounds of its workgroups.
+// step hardly depends on how many tiles there are: w4_few is faster for less than two rounds of its workgroups (17 to 32 rows of 8192 features and
+// 782 tiles of classes are three, and still go there: 45 us where w4_tiles takes 39).
+// What w4_stream takes is bounded by LDS, which holds the features of all rows: 19 rows of 4096, 9 of 8192.  One more row, on another kernel,
+// takes up to 1.6 times as long; features in pieces would move that border.
 enum W4Way { W4_STREAM, W4_FEW, W4_TILES };
 struct W4Plan {
     W4Way way;
